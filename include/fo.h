@@ -510,6 +510,147 @@ fo_status fo_run_overlapped_noalloc(const fo_plan* plan, const void* dev_plan,
                                     void* gemm_stream, void* comm_stream,
                                     const fo_options* options);
 
+/* ---- row operators ------------------------------------------------------
+ *
+ * What stands before and behind the path in a training or serving step: layer
+ * norm / RMS norm with its backward pass, activations kept in 8 bits for the
+ * backward pass, and a mixture-of-experts block's tokens, sorted by expert ahead
+ * of the experts' products and their All-to-All and combined behind them. They
+ * need no plan.
+ *
+ * Matrices of 16-bit values (dtype: fo_dtype) are row-major with rows `ld`
+ * elements apart (ld >= the row's length; 2-byte aligned, any length, odd ones
+ * included). Sums are in fp32 and results are rounded once. One call is one or
+ * two launches on `stream`, safe to capture; equal calls give equal bits. Sizes
+ * of zero are accepted. FO_ERR_SHAPE: more rows than one launch takes (2^32
+ * work-items).
+ */
+
+typedef enum { FO_NORM_LAYER = 0, FO_NORM_RMS = 1 } fo_norm;
+
+/* Checkpoint formats. A matrix of N columns is kept in blocks of FO_PACK_BLOCK
+ * values along a row, each with a scale 2^s: value = code * 2^s. With 2^e the
+ * largest power of two that is not above the block's largest magnitude:
+ *   INT8: s = e - 6; code = x / 2^s rounded to nearest even, kept within
+ *         [-127, 127]. Off by at most 2^(s-1) = 2^(e-7); fp16 values above
+ *         127.5 * 2^s by less than 2^s.
+ *   E4M3: s = e - 8, or e - 7 where the largest magnitude exceeds 1.75 * 2^e;
+ *         code = x / 2^s rounded to nearest even (OCP e4m3). Off by at most 2^-4
+ *         of the value, or 2^(s-10) where that is more.
+ * s is at least -126 (smaller blocks are rounded on that scale's grid), and no
+ * value is rounded up past the largest finite one of its dtype. A block with an
+ * infinity or a NaN reads as NaN throughout.
+ * Storage: `packed`, [M][B * 32] bytes with B = ceil(N / 32) (16-byte aligned;
+ * codes behind the row's end are 0), and `scales`, [M][B] bytes, s + 127 (255: NaN). */
+typedef enum { FO_PACK_INT8 = 0, FO_PACK_E4M3 = 1 } fo_pack_format;
+#define FO_PACK_BLOCK 32
+
+fo_status fo_pack_rows(int32_t dtype, int32_t format, int64_t M, int64_t N, const void* x, int64_t ldx,
+                       void* packed, void* scales, void* stream);
+/* out[i, n] = the value that the checkpoint stands for, rounded to dtype (exact but
+ * for fp16 values below 2^-14). */
+fo_status fo_unpack_rows(int32_t dtype, int32_t format, int64_t M, int64_t N, const void* packed,
+                         const void* scales, void* out, int64_t ldo, void* stream);
+
+/*
+ * fo_norm_forward -- per row of x [M, N], N <= 32768 (else FO_ERR_UNSUPPORTED):
+ *   mean = sum(x) / N (RMS norm: 0), rstd = 1 / sqrt(sum((x - mean)^2) / N + eps),
+ *   y = (x - mean) * rstd * gamma + beta.
+ * gamma, beta: [N] of dtype, NULL = 1 and 0. mean, rstd: [M] fp32 outputs for the
+ * backward pass, or NULL. packed and scales: a checkpoint of x for the backward
+ * pass, written on the way (both or neither). y may be x (same ld); otherwise the
+ * buffers must not overlap. Magnitudes up to 2^60 stay within fp32 on the way.
+ * Errors: FO_ERR_ARG, FO_ERR_UNSUPPORTED, FO_ERR_SHAPE, FO_ERR_HIP.
+ */
+fo_status fo_norm_forward(int32_t kind, int32_t dtype, int64_t M, int64_t N, const void* x, int64_t ldx,
+                          const void* gamma, const void* beta, float eps, void* y, int64_t ldy, float* mean,
+                          float* rstd, void* packed, void* scales, int32_t format, void* stream);
+
+/*
+ * fo_norm_backward -- the gradients of fo_norm_forward. With h = (x - mean) * rstd
+ * and g = dy * gamma:
+ *   dx = rstd * (g - sum(g) / N - h * sum(g * h) / N)   (RMS norm: without sum(g)),
+ *   dgamma[n] = sum over rows of dy * h,   dbeta[n] = sum over rows of dy.
+ * x, or packed and scales (a checkpoint of x): one of the two. mean (layer norm)
+ * and rstd as the forward pass gave them. dx [M, N] of dtype, dgamma and dbeta [N]
+ * fp32: each may be NULL, not all. dx may be dy or x (same ld). dgamma and dbeta
+ * are overwritten (zeros for M = 0) and need a workspace of
+ * fo_norm_workspace_bytes(M, N) bytes, 16-byte aligned, that no other call uses
+ * meanwhile (its contents do not matter; a graph keeps using it on replay).
+ */
+int64_t fo_norm_workspace_bytes(int64_t M, int64_t N);
+fo_status fo_norm_backward(int32_t kind, int32_t dtype, int64_t M, int64_t N, const void* dy, int64_t lddy,
+                           const void* x, int64_t ldx, const void* packed, const void* scales, int32_t format,
+                           const void* gamma, const float* mean, const float* rstd, void* dx, int64_t lddx,
+                           float* dgamma, float* dbeta, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * fo_route_sort -- the router's choices, T tokens of K experts each, in the order
+ * of experts. ids: [T, K], int32 or int64 (id_bytes 4 or 8); an id outside [0, E)
+ * is a dropped choice. Pair p = t * K + k is choice k of token t.
+ *   counts[e]   [E] pairs of expert e;
+ *   offsets[e]  [E + 1] expert e's first row; each expert has its count rounded up
+ *               to a multiple of `align` (a tile height of the GEMM that follows,
+ *               or 1), and offsets[E] rows are used in all;
+ *   slot_of[p]  [T, K] the row of pair p, -1 if dropped; an expert's pairs keep
+ *               their order;
+ *   pair_of[r]  [capacity] or NULL: the pair of row r, -1 for padding; rows behind
+ *               offsets[E] are left as they were.
+ * capacity: fo_route_capacity(T, K, E, align) at least (the rows of the worst
+ * case: T * K + min(E, T * K) * (align - 1)). K <= FO_ROUTE_MAX_CHOICES,
+ * E <= FO_ROUTE_MAX_EXPERTS. workspace: fo_route_workspace_bytes(T, K, E) bytes
+ * (0 for a few thousand pairs), 4-byte aligned, not shared with a concurrent call.
+ * The same expert may be chosen twice by a token: each choice has a row.
+ */
+#define FO_ROUTE_MAX_CHOICES 64
+#define FO_ROUTE_MAX_EXPERTS 1024
+int64_t fo_route_capacity(int64_t T, int32_t K, int32_t E, int32_t align);
+int64_t fo_route_workspace_bytes(int64_t T, int32_t K, int32_t E);
+fo_status fo_route_sort(const void* ids, int32_t id_bytes, int64_t T, int32_t K, int32_t E, int32_t align,
+                        int32_t* offsets, int32_t* counts, int32_t* slot_of, int32_t* pair_of, int64_t capacity,
+                        void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * fo_route_permute -- rows[slot_of[t, k]] = x[t] for every pair whose slot is in
+ * [0, capacity); others are skipped. x [T, H], rows [capacity, H]. With offsets and
+ * counts (both or neither; [E + 1] and [E]) the padding rows between an expert's
+ * last row and the next expert's first are zeroed; rows behind offsets[E] are left
+ * as they were. rows must not overlap x.
+ * Its backward pass is fo_route_combine without weights, of rows' gradient.
+ */
+fo_status fo_route_permute(int32_t dtype, int64_t T, int32_t K, int64_t H, const void* x, int64_t ldx,
+                           const int32_t* slot_of, void* rows, int64_t ldr, int64_t capacity,
+                           const int32_t* offsets, const int32_t* counts, int32_t E, void* stream);
+
+/*
+ * fo_route_combine -- out[t] = sum over k of weights[t, k] * rows[slot_of[t, k]]
+ * over the pairs whose slot is in [0, capacity), in the order of k, in fp32; a
+ * token without any gets zeros, and nothing is read for a dropped pair. weights:
+ * [T, K] fp32, NULL = 1. packed and scales: a checkpoint of the rows that are
+ * read ([capacity][B * 32] and [capacity][B]; other rows of it are left as they
+ * were), written on the way, or NULL; the slots must then differ from pair to pair
+ * (as fo_route_sort's do). out must not overlap rows.
+ */
+fo_status fo_route_combine(int32_t dtype, int64_t T, int32_t K, int64_t H, const void* rows, int64_t ldr,
+                           int64_t capacity, const int32_t* slot_of, const float* weights, void* out, int64_t ldo,
+                           void* packed, void* scales, int32_t format, void* stream);
+
+/*
+ * fo_route_combine_backward -- the gradients of fo_route_combine:
+ *   drows[slot_of[t, k]] = weights[t, k] * dout[t],
+ *   dweights[t, k] = sum over h of dout[t, h] * rows[slot_of[t, k], h],
+ * 0 for dropped pairs. drows [capacity, H] of dtype and dweights [T, K] fp32: one
+ * of the two may be NULL. dweights reads rows or a checkpoint of them (one of the
+ * two; neither without dweights). The slots must differ from pair to pair.
+ * Padding rows of drows are zeroed as in fo_route_permute, the others left as
+ * they were. drows may be rows (same ld).
+ */
+fo_status fo_route_combine_backward(int32_t dtype, int64_t T, int32_t K, int64_t H, const void* dout, int64_t lddo,
+                                    const void* rows, int64_t ldr, const void* packed, const void* scales,
+                                    int32_t format, int64_t capacity, const int32_t* slot_of, const float* weights,
+                                    void* drows, int64_t lddr, float* dweights, const int32_t* offsets,
+                                    const int32_t* counts, int32_t E, void* stream);
+
 /*
  * How the producer (GEMM epilogue) publishes a finished tile and how the
  * consumer reads a signalled group. All modes are correct; they differ in

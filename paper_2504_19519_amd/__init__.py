@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import sys
 from typing import Optional, Sequence
 
 import numpy as np
@@ -23,6 +24,9 @@ __all__ = [
     "get_poll_timeout_us", "device_num_cus", "set_sync_mode", "get_sync_mode",
     "set_consumer_grid", "get_consumer_grid", "Options", "options", "device_wall_clock_khz", "LIB_PATH",
     "FP16", "BF16", "TILE", "SUBTILE", "SUBTOKEN", "ROWMAJOR",
+    "norm_forward", "norm_backward", "norm_workspace_bytes", "pack_rows", "unpack_rows", "packed_bytes",
+    "route_sort", "route_permute", "route_combine", "route_combine_backward", "route_capacity",
+    "route_workspace_bytes", "LAYER_NORM", "RMS_NORM", "PACK_INT8", "PACK_E4M3",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libfo.so")
@@ -133,6 +137,23 @@ def lib() -> ctypes.CDLL:
     L.fo_set_poll_timeout_us.argtypes = [i64]
     L.fo_get_poll_timeout_us.restype = i64
     L.fo_device_num_cus.argtypes = [i32, pi32]
+    f32 = ctypes.c_float
+    L.fo_norm_forward.argtypes = [i32, i32, i64, i64, vp, i64, vp, vp, f32, vp, i64, vp, vp, vp, vp, i32, vp]
+    L.fo_norm_backward.argtypes = [i32, i32, i64, i64, vp, i64, vp, i64, vp, vp, i32, vp, vp, vp, vp, i64, vp, vp,
+                                   vp, i64, vp]
+    L.fo_norm_workspace_bytes.argtypes, L.fo_norm_workspace_bytes.restype = [i64, i64], i64
+    L.fo_pack_rows.argtypes = [i32, i32, i64, i64, vp, i64, vp, vp, vp]
+    L.fo_unpack_rows.argtypes = [i32, i32, i64, i64, vp, vp, vp, i64, vp]
+    L.fo_route_capacity.argtypes, L.fo_route_capacity.restype = [i64, i32, i32, i32], i64
+    L.fo_route_workspace_bytes.argtypes, L.fo_route_workspace_bytes.restype = [i64, i32, i32], i64
+    L.fo_route_sort.argtypes = [vp, i32, i64, i32, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp]
+    L.fo_route_permute.argtypes = [i32, i64, i32, i64, vp, i64, vp, vp, i64, i64, vp, vp, i32, vp]
+    L.fo_route_combine.argtypes = [i32, i64, i32, i64, vp, i64, i64, vp, vp, vp, i64, vp, vp, i32, vp]
+    L.fo_route_combine_backward.argtypes = [i32, i64, i32, i64, vp, i64, vp, i64, vp, vp, i32, i64, vp, vp, vp, i64,
+                                            vp, vp, vp, i32, vp]
+    for f in (L.fo_norm_forward, L.fo_norm_backward, L.fo_pack_rows, L.fo_unpack_rows, L.fo_route_sort,
+              L.fo_route_permute, L.fo_route_combine, L.fo_route_combine_backward):
+        f.restype = ctypes.c_int
     L.fo_status_string.argtypes, L.fo_status_string.restype = [ctypes.c_int], ctypes.c_char_p
     L.fo_last_error.restype = ctypes.c_char_p
     for f in (L.fo_plan_cache_create, L.fo_plan_cache_add, L.fo_plan_cache_lookup, L.fo_plan_cache_entry):
@@ -547,3 +568,234 @@ def device_num_cus(device: int = 0) -> int:
     v = ctypes.c_int32()
     _check(lib().fo_device_num_cus(device, ctypes.byref(v)))
     return int(v.value)
+
+
+# ---- row operators ----------------------------------------------------------
+
+LAYER_NORM, RMS_NORM = 0, 1                  # fo_norm
+PACK_INT8, PACK_E4M3 = 0, 1                  # fo_pack_format
+PACK_BLOCK = 32                              # FO_PACK_BLOCK
+_NORMS = {"layer": LAYER_NORM, "rms": RMS_NORM, LAYER_NORM: LAYER_NORM, RMS_NORM: RMS_NORM}
+_FORMATS = {"int8": PACK_INT8, "e4m3": PACK_E4M3, PACK_INT8: PACK_INT8, PACK_E4M3: PACK_E4M3}
+
+
+def _pick(table, key, what: str) -> int:
+    try:
+        return table[key]
+    except (KeyError, TypeError):
+        raise ValueError(f"{what}: one of {[k for k in table if isinstance(k, str)]}, got {key!r}") from None
+
+
+class _Args:
+    """Pointers of one row operator's arguments. Tensors are checked: on one GPU,
+    the current one (and the stream's), of the element size and dtype that the call
+    takes, large enough, and contiguous or (matrices) with rows of unit stride. Raw
+    pointers are taken as given."""
+
+    __slots__ = ("dtype", "device")
+
+    def __init__(self, dtype, stream):
+        self.dtype = _pick(_DTYPES, dtype, "dtype")
+        self.device = getattr(stream, "device_index", None)
+        if self.device is None:
+            torch = sys.modules.get("torch")
+            if torch is not None and torch.cuda.is_initialized():
+                self.device = torch.cuda.current_device()
+
+    def _on_device(self, x, what):
+        d = x.get_device()
+        if d < 0:
+            raise ValueError(f"{what}: a tensor on the GPU is needed")
+        if self.device is None:
+            self.device = d
+        elif d != self.device:
+            raise ValueError(f"{what}: on device {d}, the call runs on device {self.device}")
+
+    def rows(self, x, M: int, N: int, ld, what: str):
+        """(pointer, row distance) of a [M, N] matrix of 16-bit values."""
+        if x is None:
+            return None, N
+        if not hasattr(x, "get_device"):
+            return _ptr(x), N if ld is None else int(ld)
+        self._on_device(x, what)
+        if x.element_size() != 2 or self._other(x):
+            raise ValueError(f"{what}: {x.dtype} values for {'bf16' if self.dtype else 'fp16'}")
+        if ld is None and x.dim() == 2 and x.shape[1] == N:
+            if x.shape[0] < M:
+                raise ValueError(f"{what}: {x.shape[0]} rows, the call needs {M}")
+            step, unit = x.stride()
+            if (unit != 1 and N > 1) or (step < N and M > 1):
+                raise ValueError(f"{what}: rows of unit stride that do not overlap are needed, strides are "
+                                 f"{tuple(x.stride())}")
+            return x.data_ptr(), step if M > 1 else N
+        ld = N if ld is None else int(ld)
+        need = (M - 1) * ld + N if M > 0 and N > 0 else 0
+        if not x.is_contiguous() or x.numel() < need:
+            raise ValueError(f"{what}: {need} contiguous elements are needed, or a [{M}, {N}] view")
+        return x.data_ptr(), ld
+
+    def _other(self, x) -> bool:
+        """Whether x holds the other 16-bit floating type (integer containers fit both)."""
+        return x.is_floating_point() and (str(x.dtype) == "torch.bfloat16") != (self.dtype == BF16)
+
+    def flat(self, x, count: int, what: str, size: int = 4, floating=None):
+        """Pointer of `count` contiguous elements of `size` bytes."""
+        if x is None:
+            return None
+        if not hasattr(x, "get_device"):
+            return _ptr(x)
+        self._on_device(x, what)
+        if x.element_size() != size or (floating is not None and x.is_floating_point() != floating) or (
+                size == 2 and self._other(x)):
+            raise ValueError(f"{what}: elements of {x.dtype}")
+        if not x.is_contiguous() or x.numel() < count:
+            raise ValueError(f"{what}: {count} contiguous elements are needed")
+        return x.data_ptr()
+
+    def space(self, x, what: str = "workspace"):
+        """(pointer, bytes) of a workspace; a raw pointer's size is not known and taken as enough."""
+        if x is None:
+            return None, 0
+        if not hasattr(x, "get_device"):
+            return _ptr(x), (1 << 63) - 1
+        self._on_device(x, what)
+        if not x.is_contiguous():
+            raise ValueError(f"{what}: contiguous memory is needed")
+        return x.data_ptr(), x.numel() * x.element_size()
+
+    def pack(self, packed, scales, M: int, N: int, fmt):
+        """(packed, scales, format) of an [M, N] checkpoint."""
+        if packed is None and scales is None:
+            return None, None, 0
+        codes, steps = packed_bytes(M, N)
+        return (self.flat(packed, codes, "packed", 1, False), self.flat(scales, steps, "scales", 1, False),
+                _pick(_FORMATS, fmt, "fmt"))
+
+
+def packed_bytes(M: int, N: int):
+    """(bytes of `packed`, bytes of `scales`) of an [M, N] checkpoint."""
+    blocks = -(-N // PACK_BLOCK)
+    return M * blocks * PACK_BLOCK, M * blocks
+
+
+def norm_workspace_bytes(M: int, N: int) -> int:
+    """fo_norm_workspace_bytes: what norm_backward needs for dgamma and dbeta."""
+    return lib().fo_norm_workspace_bytes(M, N)
+
+
+def norm_forward(kind, x, gamma, beta, y, M: int, N: int, dtype, eps: float = 1e-6, mean=None, rstd=None,
+                 packed=None, scales=None, fmt="int8", ldx=None, ldy=None, stream=None) -> None:
+    """fo_norm_forward: y = (x - mean) * rstd * gamma + beta per row (kind "layer";
+    "rms": mean = 0). mean, rstd ([M] fp32) and packed, scales (a checkpoint of x in
+    the format fmt) are written for norm_backward when given."""
+    a = _Args(dtype, stream)
+    px, sx = a.rows(x, M, N, ldx, "x")
+    py, sy = a.rows(y, M, N, ldy, "y")
+    codes, steps, fmt = a.pack(packed, scales, M, N, fmt)
+    _check(lib().fo_norm_forward(_pick(_NORMS, kind, "kind"), a.dtype, M, N, px, sx, a.flat(gamma, N, "gamma", 2),
+                                 a.flat(beta, N, "beta", 2), eps, py, sy, a.flat(mean, M, "mean", 4, True),
+                                 a.flat(rstd, M, "rstd", 4, True), codes, steps, fmt, _stream(stream)))
+
+
+def norm_backward(kind, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, M: int, N: int, dtype, workspace=None,
+                  packed=None, scales=None, fmt="int8", lddy=None, ldx=None, lddx=None, stream=None) -> None:
+    """fo_norm_backward: the gradients of norm_forward, from x (None with a
+    checkpoint: packed, scales, fmt). dx, dgamma, dbeta (fp32) may be None."""
+    a = _Args(dtype, stream)
+    pg, sg = a.rows(dy, M, N, lddy, "dy")
+    px, sx = a.rows(x, M, N, ldx, "x")
+    pd, sd = a.rows(dx, M, N, lddx, "dx")
+    codes, steps, fmt = a.pack(packed, scales, M, N, fmt)
+    work, size = a.space(workspace)
+    _check(lib().fo_norm_backward(_pick(_NORMS, kind, "kind"), a.dtype, M, N, pg, sg, px, sx, codes, steps, fmt,
+                                  a.flat(gamma, N, "gamma", 2), a.flat(mean, M, "mean", 4, True),
+                                  a.flat(rstd, M, "rstd", 4, True), pd, sd, a.flat(dgamma, N, "dgamma", 4, True),
+                                  a.flat(dbeta, N, "dbeta", 4, True), work, size, _stream(stream)))
+
+
+def pack_rows(x, packed, scales, M: int, N: int, dtype, fmt="int8", ldx=None, stream=None) -> None:
+    """fo_pack_rows: x [M, N] kept in 8 bits (packed_bytes(M, N) bytes)."""
+    a = _Args(dtype, stream)
+    px, sx = a.rows(x, M, N, ldx, "x")
+    codes, steps, f = a.pack(packed, scales, M, N, fmt)
+    _check(lib().fo_pack_rows(a.dtype, f, M, N, px, sx, codes, steps, _stream(stream)))
+
+
+def unpack_rows(packed, scales, out, M: int, N: int, dtype, fmt="int8", ldo=None, stream=None) -> None:
+    """fo_unpack_rows: the values that a checkpoint stands for."""
+    a = _Args(dtype, stream)
+    po, so = a.rows(out, M, N, ldo, "out")
+    codes, steps, f = a.pack(packed, scales, M, N, fmt)
+    _check(lib().fo_unpack_rows(a.dtype, f, M, N, codes, steps, po, so, _stream(stream)))
+
+
+def route_capacity(T: int, K: int, E: int, align: int = 1) -> int:
+    """fo_route_capacity: rows that hold T * K pairs however they fall."""
+    return lib().fo_route_capacity(T, K, E, align)
+
+
+def route_workspace_bytes(T: int, K: int, E: int) -> int:
+    """fo_route_workspace_bytes: what route_sort needs (0: nothing)."""
+    return lib().fo_route_workspace_bytes(T, K, E)
+
+
+def route_sort(ids, T: int, K: int, E: int, offsets, counts, slot_of, pair_of=None, workspace=None, align: int = 1,
+               id_bytes=None, capacity=None, stream=None) -> None:
+    """fo_route_sort: the router's choices ids [T, K] (int32 or int64; outside
+    [0, E): dropped) in the order of experts. Writes offsets [E + 1], counts [E],
+    slot_of [T, K] and, if given, pair_of (capacity rows: its length unless given).
+    id_bytes (4 or 8) is only needed for a raw pointer."""
+    a = _Args(FP16, stream)
+    size = ids.element_size() if hasattr(ids, "element_size") else 4 if id_bytes is None else int(id_bytes)
+    rows = int(capacity) if capacity is not None else pair_of.numel() if hasattr(pair_of, "numel") else \
+        route_capacity(T, K, E, align)
+    work, nbytes = a.space(workspace)
+    _check(lib().fo_route_sort(a.flat(ids, T * K, "ids", size, False), size, T, K, E, align,
+                               a.flat(offsets, E + 1, "offsets", 4, False), a.flat(counts, E, "counts", 4, False),
+                               a.flat(slot_of, T * K, "slot_of", 4, False), a.flat(pair_of, rows, "pair_of", 4, False),
+                               rows, work, nbytes, _stream(stream)))
+
+
+def route_permute(x, slot_of, rows, T: int, K: int, H: int, dtype, capacity: int, offsets=None, counts=None,
+                  E: int = 0, ldx=None, ldr=None, stream=None) -> None:
+    """fo_route_permute: rows[slot_of[t, k]] = x[t]; padding rows are zeroed where
+    offsets [E + 1] and counts [E] are given."""
+    a = _Args(dtype, stream)
+    px, sx = a.rows(x, T, H, ldx, "x")
+    pr, sr = a.rows(rows, capacity, H, ldr, "rows")
+    _check(lib().fo_route_permute(a.dtype, T, K, H, px, sx, a.flat(slot_of, T * K, "slot_of", 4, False), pr, sr,
+                                  capacity, a.flat(offsets, E + 1, "offsets", 4, False),
+                                  a.flat(counts, E, "counts", 4, False), E, _stream(stream)))
+
+
+def route_combine(rows, slot_of, weights, out, T: int, K: int, H: int, dtype, capacity: int, packed=None, scales=None,
+                  fmt="int8", ldr=None, ldo=None, stream=None) -> None:
+    """fo_route_combine: out[t] = sum over k of weights[t, k] * rows[slot_of[t, k]]
+    (weights None: 1). packed, scales: a checkpoint of the rows, written for
+    route_combine_backward."""
+    a = _Args(dtype, stream)
+    pr, sr = a.rows(rows, capacity, H, ldr, "rows")
+    po, so = a.rows(out, T, H, ldo, "out")
+    codes, steps, fmt = a.pack(packed, scales, capacity, H, fmt)
+    _check(lib().fo_route_combine(a.dtype, T, K, H, pr, sr, capacity, a.flat(slot_of, T * K, "slot_of", 4, False),
+                                  a.flat(weights, T * K, "weights", 4, True), po, so, codes, steps, fmt,
+                                  _stream(stream)))
+
+
+def route_combine_backward(dout, rows, slot_of, weights, drows, dweights, T: int, K: int, H: int, dtype, capacity: int,
+                           offsets=None, counts=None, E: int = 0, packed=None, scales=None, fmt="int8", lddo=None,
+                           ldr=None, lddr=None, stream=None) -> None:
+    """fo_route_combine_backward: drows[slot_of[t, k]] = weights[t, k] * dout[t] and
+    dweights[t, k] = <dout[t], rows[slot_of[t, k]]>, the rows themselves or a
+    checkpoint of them (rows None). drows or dweights may be None."""
+    a = _Args(dtype, stream)
+    pg, sg = a.rows(dout, T, H, lddo, "dout")
+    pr, sr = a.rows(rows, capacity, H, ldr, "rows")
+    pd, sd = a.rows(drows, capacity, H, lddr, "drows")
+    codes, steps, fmt = a.pack(packed, scales, capacity, H, fmt)
+    _check(lib().fo_route_combine_backward(a.dtype, T, K, H, pg, sg, pr, sr, codes, steps, fmt, capacity,
+                                           a.flat(slot_of, T * K, "slot_of", 4, False),
+                                           a.flat(weights, T * K, "weights", 4, True), pd, sd,
+                                           a.flat(dweights, T * K, "dweights", 4, True),
+                                           a.flat(offsets, E + 1, "offsets", 4, False),
+                                           a.flat(counts, E, "counts", 4, False), E, _stream(stream)))

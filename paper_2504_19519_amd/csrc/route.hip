@@ -1,0 +1,358 @@
+// Tokens sorted by expert and back (the two sides of an All-to-All between a
+// router and its experts).
+//
+// Sort: a stable counting sort of the pairs (token t, choice k), p = t K + k, by
+// expert. A workgroup takes a run of pairs, each of its waves a part of the
+// run: the parts' counts per expert (LDS) summed up in order give each part's
+// first place with each expert, and within a wave the lanes of one expert find
+// each other by ballots, so that a pair's place is a sum of counts and no
+// atomic's order shows. Several workgroups: a first launch writes their counts,
+// which every workgroup of the second one adds up.
+//
+// Permute, combine and the combine's backward pass move whole rows of H values
+// and are bound by memory: each row is read once (a token's row stays in
+// registers while it goes to its K places, a token's K rows are in flight
+// together).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "rowops.h"
+#include "rows.h"
+
+namespace fo {
+namespace {
+
+constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64;
+constexpr int64_t kSortRun = 8192;          // pairs of one workgroup, at least
+constexpr int kSortBlocks = 256;            // workgroups, at most
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+
+template <typename ID>
+__device__ __forceinline__ int expert_of(const ID* ids, int64_t p, int64_t end, int experts) {
+    if (p >= end) return -1;
+    const ID e = ids[p];
+    return e >= 0 && e < (ID)experts ? (int)e : -1;
+}
+
+template <typename ID>
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs a, int64_t run) {
+    __shared__ int32_t s_count[kMaxExperts];
+    for (int e = threadIdx.x; e < a.experts; e += kSortThreads) s_count[e] = 0;
+    __syncthreads();
+    const int64_t first = blockIdx.x * run, end = first + run < a.pairs ? first + run : a.pairs;
+    for (int64_t p = first + threadIdx.x; p < end; p += kSortThreads) {
+        const int e = expert_of(static_cast<const ID*>(a.ids), p, end, a.experts);
+        if (e >= 0) atomicAdd(&s_count[e], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.experts; e += kSortThreads) a.hist[(int64_t)blockIdx.x * a.experts + e] = s_count[e];
+}
+
+template <typename ID>
+__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs a, int64_t run) {
+    __shared__ int32_t s_place[kSortWaves][kMaxExperts];
+    __shared__ int32_t s_first[kMaxExperts], s_total[kMaxExperts], s_wave[kSortWaves];
+    const ID* ids = static_cast<const ID*>(a.ids);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, E = a.experts;
+    const int64_t first = blockIdx.x * run, end = first + run < a.pairs ? first + run : a.pairs;
+    const int64_t part = run / kSortWaves, begin = first + wave * part;
+    const int64_t stop = begin + part < end ? begin + part : end;
+
+    for (int i = threadIdx.x; i < kSortWaves * E; i += kSortThreads) s_place[i / E][i % E] = 0;
+    __syncthreads();
+    for (int64_t p = begin + lane; p < stop; p += 64) {
+        const int e = expert_of(ids, p, stop, E);
+        if (e >= 0) atomicAdd(&s_place[wave][e], 1);
+    }
+    __syncthreads();
+    // per expert: the parts' counts to their first places within the expert
+    for (int e = threadIdx.x; e < E; e += kSortThreads) {
+        int32_t before = 0, total = 0;
+        if (gridDim.x > 1) {
+            for (uint32_t b = 0; b < gridDim.x; ++b) {
+                const int32_t n = a.hist[(int64_t)b * E + e];
+                before += b < blockIdx.x ? n : 0;
+                total += n;
+            }
+        }
+        int32_t at = before;
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int32_t n = s_place[w][e];
+            s_place[w][e] = at;
+            at += n;
+        }
+        s_total[e] = gridDim.x > 1 ? total : at;
+    }
+    __syncthreads();
+    // the experts' first rows: two experts per thread, padded counts summed up
+    {
+        int32_t mine[2], sum = 0;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int e = 2 * threadIdx.x + j;
+            mine[j] = sum;
+            if (e < E) sum += (int32_t)(((int64_t)s_total[e] + a.align - 1) / a.align * a.align);
+        }
+        int32_t scan = sum;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int32_t up = __shfl_up(scan, off, 64);
+            if (lane >= off) scan += up;
+        }
+        if (lane == 63) s_wave[wave] = scan;
+        __syncthreads();
+        int32_t base = scan - sum;
+        for (int w = 0; w < wave; ++w) base += s_wave[w];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int e = 2 * threadIdx.x + j;
+            if (e < E) s_first[e] = base + mine[j];
+            if (blockIdx.x == 0) {
+                if (e < E) {
+                    a.offsets[e] = base + mine[j];
+                    a.counts[e] = s_total[e];
+                }
+                if (e == E - 1) a.offsets[E] = base + sum;
+            }
+        }
+    }
+    __syncthreads();
+    // padding rows belong to no pair
+    if (a.pair_of) {
+        for (int e = blockIdx.x; e < E; e += gridDim.x) {
+            const int32_t from = s_first[e] + s_total[e];
+            const int32_t to = s_first[e] + (int32_t)(((int64_t)s_total[e] + a.align - 1) / a.align * a.align);
+            for (int32_t r = from + threadIdx.x; r < to; r += kSortThreads) a.pair_of[r] = -1;
+        }
+    }
+    int bits = 0;
+    while ((1 << bits) < E) ++bits;
+    volatile int32_t* place = s_place[wave];
+    for (int64_t p0 = begin; p0 < stop; p0 += 64) {
+        const int64_t p = p0 + lane;
+        const int e = expert_of(ids, p, stop, E);
+        uint64_t same = __ballot(e >= 0);
+        for (int b = 0; b < bits; ++b) {
+            const uint64_t set = __ballot((e >> b) & 1);
+            same &= ((e >> b) & 1) ? set : ~set;
+        }
+        if (e >= 0) {
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            const int32_t slot = s_first[e] + place[e] + rank;
+            a.slot_of[p] = slot;
+            if (a.pair_of) a.pair_of[slot] = (int32_t)p;
+        } else if (p < stop) {
+            a.slot_of[p] = -1;
+        }
+        __builtin_amdgcn_wave_barrier();
+        // the last lane of each expert moves its part's place on
+        if (e >= 0 && (same >> lane) == 1ull) place[e] = place[e] + __popcll(same);
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// A wave's (token, slice of 64 chunks) in a grid of T tokens of `slices`.
+struct Unit {
+    int32_t t, s;
+};
+__device__ __forceinline__ Unit unit_of(uint32_t slices) {
+    const uint32_t u = blockIdx.x * kWaves + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Unit r;
+    r.t = (int32_t)(u / slices);
+    r.s = (int32_t)(u - (uint32_t)r.t * slices);
+    return r;
+}
+
+// Rows between an expert's last and the next expert's first are zeroed: `per`
+// workgroups per expert, a wave per row at a time.
+__device__ __forceinline__ void zero_padding(const RouteArgs& a, uint16_t* rows, int64_t ld, uint32_t block, int per) {
+    const int e = (int)(block / (uint32_t)per), lane = threadIdx.x & 63;
+    const int wave = (int)(block % (uint32_t)per) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int32_t from = a.offsets[e] + a.counts[e], to = a.offsets[e + 1];
+    from = from < 0 ? 0 : from;
+    to = to > a.capacity ? a.capacity : to;
+    const int full = (int)(a.H >> 3), tail = (int)(a.H & 7);
+    for (int64_t r = (int64_t)from + wave; r < to; r += per * kWaves) {
+        uint16_t* row = rows + r * ld;
+        for (int c = lane; c < full; c += 64) store8(row + 8 * (int64_t)c, u32x4_t{0u, 0u, 0u, 0u});
+        if (lane < tail) row[8 * (int64_t)full + lane] = 0;
+    }
+}
+
+__device__ __forceinline__ bool is_row(const RouteArgs& a, int32_t slot) { return slot >= 0 && slot < a.capacity; }
+
+__global__ __launch_bounds__(kThreads) void permute_kernel(const RouteArgs a, uint32_t slices, uint32_t blocks, int per) {
+    if (blockIdx.x >= blocks) return zero_padding(a, a.rows, a.ldr, blockIdx.x - blocks, per);
+    const Unit u = unit_of(slices);
+    if (u.t >= a.T) return;
+    const int lane = threadIdx.x & 63, full = (int)(a.H >> 3), tail = (int)(a.H & 7), c = u.s * 64 + lane;
+    const uint16_t* row = a.x + u.t * a.ldx;
+    const bool has_tail = u.s == (int)slices - 1 && lane < tail;
+    u32x4_t v{};
+    uint16_t vt = 0;
+    if (c < full) v = load8(row + 8 * (int64_t)c);
+    if (has_tail) vt = row[8 * (int64_t)full + lane];
+    for (int k = 0; k < a.K; ++k) {
+        const int32_t slot = a.slot_of[(int64_t)u.t * a.K + k];
+        if (!is_row(a, slot)) continue;
+        uint16_t* out = a.rows + slot * a.ldr;
+        if (c < full) store8(out + 8 * (int64_t)c, v);
+        if (has_tail) out[8 * (int64_t)full + lane] = vt;
+    }
+}
+
+// FMT: -1, or the format of the checkpoint that the rows are packed into.
+template <int DT, int FMT>
+__global__ __launch_bounds__(kThreads) void combine_kernel(const RouteArgs a, uint32_t slices) {
+    const Unit u = unit_of(slices);
+    if (u.t >= a.T) return;
+    const int lane = threadIdx.x & 63, full = (int)(a.H >> 3), tail = (int)(a.H & 7), c = u.s * 64 + lane;
+    const bool has_tail = u.s == (int)slices - 1 && lane < tail;
+    float sum[8] = {}, sum_t = 0.0f;
+    for (int k = 0; k < a.K; ++k) {
+        const int64_t p = (int64_t)u.t * a.K + k;
+        const int32_t slot = a.slot_of[p];
+        if (!is_row(a, slot)) continue;
+        const float w = a.weights ? a.weights[p] : 1.0f;
+        const uint16_t* row = a.rows + slot * a.ldr;
+        u32x4_t v{};
+        if (c < full) v = load8(row + 8 * (int64_t)c);
+        float f[8];
+        widen<DT>(v, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += w * f[e];
+        if (has_tail) sum_t += w * to_f32<DT>(row[8 * (int64_t)full + lane]);
+        if constexpr (FMT >= 0) {
+            const int64_t blocks = (a.H + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK;
+            uint8_t* packed = a.packed + slot * blocks * FO_PACK_BLOCK;
+            uint8_t* scales = a.scales + slot * blocks;
+            if (c < a.H / FO_PACK_BLOCK * 4) pack_chunk<DT, FMT>(v, c, packed, scales);
+            if (u.s == (int)slices - 1 && a.H % FO_PACK_BLOCK) pack_last<DT, FMT>(row, a.H, lane, packed, scales);
+        }
+    }
+    uint16_t* out = a.out + u.t * a.ldo;
+    if (c < full) store8(out + 8 * (int64_t)c, narrow<DT>(sum));
+    if (has_tail) out[8 * (int64_t)full + lane] = (uint16_t)from_f32<DT>(sum_t);
+}
+
+// A wave per pair: drows[slot] = w dout[t] and dw = <dout[t], rows[slot]>. SRC: where
+// the rows come from: 0 themselves, 1 + format a checkpoint of them.
+template <int DT, int SRC>
+__global__ __launch_bounds__(kThreads) void combine_backward_kernel(const RouteArgs a, uint32_t blocks, int per) {
+    if (blockIdx.x >= blocks) return zero_padding(a, a.out, a.ldo, blockIdx.x - blocks, per);
+    const int64_t p = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (p >= (int64_t)a.T * a.K) return;
+    const int lane = threadIdx.x & 63, full = (int)(a.H >> 3), tail = (int)(a.H & 7);
+    const int32_t slot = a.slot_of[p];
+    if (!is_row(a, slot)) {
+        if (lane == 0 && a.dweights) a.dweights[p] = 0.0f;
+        return;
+    }
+    const float w = a.weights ? a.weights[p] : 1.0f;
+    const int64_t blocks32 = (a.H + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK;
+    const uint16_t* grow = a.x + p / a.K * a.ldx;
+    const uint16_t* row = SRC == 0 && a.dweights ? a.rows + slot * a.ldr : nullptr;
+    const uint8_t* packed = SRC ? a.packed + slot * blocks32 * FO_PACK_BLOCK : nullptr;
+    const uint8_t* scales = SRC ? a.scales + slot * blocks32 : nullptr;
+    uint16_t* out = a.out ? a.out + slot * a.ldo : nullptr;
+    float dot = 0.0f;
+    for (int c = lane; c < full; c += 64) {
+        float g[8];
+        widen<DT>(load8(grow + 8 * (int64_t)c), g);
+        if (a.dweights) {
+            float f[8];
+            if constexpr (SRC == 0) widen<DT>(load8(row + 8 * (int64_t)c), f);
+            else decode8<SRC - 1>(*reinterpret_cast<const u32x2_t*>(packed + 8 * (int64_t)c), scale_of(scales[c >> 2]), f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dot += g[e] * f[e];
+        }
+        if (out) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] *= w;
+            store8(out + 8 * (int64_t)c, narrow<DT>(g));
+        }
+    }
+    if (lane < tail) {
+        const int64_t c = 8 * (int64_t)full + lane;
+        const float g = to_f32<DT>(grow[c]);
+        if (a.dweights) {
+            if constexpr (SRC == 0) dot += g * to_f32<DT>(row[c]);
+            else dot += g * decode1<SRC - 1>(packed[c], scale_of(scales[c / FO_PACK_BLOCK]));
+        }
+        if (out) out[c] = (uint16_t)from_f32<DT>(g * w);
+    }
+    if (a.dweights) {
+        dot = wave_sum(dot);
+        if (lane == 0) a.dweights[p] = dot;
+    }
+}
+
+uint32_t slices_of(int64_t H) { return (uint32_t)std::max<int64_t>(1, (H / 8 + 63) / 64); }
+// Workgroups per expert that zero padding rows.
+int padding_blocks(const RouteArgs& a) { return a.offsets ? std::max(1, std::min(16, 256 / a.E)) : 0; }
+
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+}  // namespace
+
+int64_t sort_blocks(int64_t pairs) {
+    return std::max<int64_t>(1, std::min<int64_t>((pairs + kSortRun - 1) / kSortRun, kSortBlocks));
+}
+
+hipError_t launch_sort(const SortArgs& a, hipStream_t s) {
+    const int64_t blocks = sort_blocks(a.pairs);
+    // whole steps of every wave
+    const int64_t run = ((a.pairs + blocks - 1) / blocks + kSortThreads - 1) / kSortThreads * kSortThreads;
+    const dim3 g((uint32_t)blocks), b(kSortThreads);
+    auto go = [&](auto id) {
+        using ID = decltype(id);
+        if (blocks > 1) hipLaunchKernelGGL(sort_count_kernel<ID>, g, b, 0, s, a, run);
+        hipLaunchKernelGGL(sort_place_kernel<ID>, g, b, 0, s, a, run);
+    };
+    if (a.id_bytes == 8) go(int64_t{});
+    else go(int32_t{});
+    return hipGetLastError();
+}
+
+hipError_t launch_permute(const RouteArgs& a, hipStream_t s) {
+    const uint32_t slices = slices_of(a.H);
+    const uint32_t blocks = (uint32_t)(((int64_t)a.T * slices + kWaves - 1) / kWaves);
+    const int per = padding_blocks(a);
+    hipLaunchKernelGGL(permute_kernel, dim3(blocks + (uint32_t)per * a.E), dim3(kThreads), 0, s, a, slices, blocks, per);
+    return hipGetLastError();
+}
+
+hipError_t launch_combine(int dtype, const RouteArgs& a, hipStream_t s) {
+    const uint32_t slices = slices_of(a.H);
+    const dim3 g((uint32_t)(((int64_t)a.T * slices + kWaves - 1) / kWaves)), b(kThreads);
+    auto from = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (!a.packed) hipLaunchKernelGGL((combine_kernel<DT, -1>), g, b, 0, s, a, slices);
+        else if (a.format == FO_PACK_INT8) hipLaunchKernelGGL((combine_kernel<DT, FO_PACK_INT8>), g, b, 0, s, a, slices);
+        else hipLaunchKernelGGL((combine_kernel<DT, FO_PACK_E4M3>), g, b, 0, s, a, slices);
+    };
+    if (dtype == FO_FP16) from(Int<FO_FP16>());
+    else from(Int<FO_BF16>());
+    return hipGetLastError();
+}
+
+hipError_t launch_combine_backward(int dtype, const RouteArgs& a, hipStream_t s) {
+    const uint32_t blocks = (uint32_t)(((int64_t)a.T * a.K + kWaves - 1) / kWaves);
+    const int per = a.out ? padding_blocks(a) : 0;
+    const dim3 g(blocks + (uint32_t)(per * a.E)), b(kThreads);
+    auto from = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (!a.packed) hipLaunchKernelGGL((combine_backward_kernel<DT, 0>), g, b, 0, s, a, blocks, per);
+        else if (a.format == FO_PACK_INT8)
+            hipLaunchKernelGGL((combine_backward_kernel<DT, 1 + FO_PACK_INT8>), g, b, 0, s, a, blocks, per);
+        else hipLaunchKernelGGL((combine_backward_kernel<DT, 1 + FO_PACK_E4M3>), g, b, 0, s, a, blocks, per);
+    };
+    if (dtype == FO_FP16) from(Int<FO_FP16>());
+    else from(Int<FO_BF16>());
+    return hipGetLastError();
+}
+
+}  // namespace fo
