@@ -5,7 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "fo.h"
+#include "fo_internal.h"
 
 namespace fo {
 
@@ -23,12 +23,13 @@ struct NormArgs {
     float* rstd;                // [M]
     uint8_t* packed;            // checkpoint, or null
     uint8_t* scales;
-    float* partial;             // backward: [blocks][2][N] sums of dy * xhat and dy, or null
+    float* partial;             // backward: [blocks][2][norm_partial_cols(N)] sums of dy * h and dy, or null
     int64_t M, N, ldx, ldy, lddx;
     float eps;
     float scale;                // forward: the largest power of two with N * scale <= 1
     int32_t layer;              // 1: layer norm, 0: RMS norm
     int32_t format;             // of the checkpoint
+    int32_t with_beta;          // backward: the sums of dy are wanted
 };
 
 // The kernel form of a norm's launch: threads of a row, chunks of eight values
@@ -38,6 +39,8 @@ struct NormForm {
     uint32_t blocks;
 };
 constexpr int64_t kMaxNormCols = 32768;
+// Columns of the partial sums: whole chunks, so that every row of them is 16-byte aligned.
+FO_HD inline int64_t norm_partial_cols(int64_t N) { return (N + 7) / 8 * 8; }
 NormForm norm_forward_form(int64_t M, int64_t N);
 NormForm norm_backward_form(int64_t M, int64_t N);
 hipError_t launch_norm_forward(int dtype, const NormArgs& a, hipStream_t s);

@@ -59,7 +59,7 @@ int64_t slices_of(int64_t n) { return std::max<int64_t>(1, (n / 8 + 63) / 64); }
 
 int64_t norm_partial_bytes(int64_t M, int64_t N) {
     const NormForm f = norm_backward_form(M, N);
-    return M > 0 && N > 0 ? (int64_t)f.blocks * f.rows * 2 * N * 4 : 0;
+    return M > 0 && N > 0 ? (int64_t)f.blocks * 2 * norm_partial_cols(N) * 4 : 0;
 }
 
 fo_status check_route(int32_t dtype, int64_t T, int32_t K, int64_t H, const void* slot_of, const void* weights,
@@ -172,6 +172,7 @@ fo_status fo_norm_backward(int32_t kind, int32_t dtype, int64_t M, int64_t N, co
     a.M = M; a.N = N; a.ldx = ldx; a.ldy = lddy; a.lddx = lddx;
     a.layer = kind == FO_NORM_LAYER;
     a.format = format;
+    a.with_beta = dbeta != nullptr;
     return fo::done(fo::launch_norm_backward(dtype, a, dgamma, dbeta, (hipStream_t)stream), "norm backward launch");
 }
 

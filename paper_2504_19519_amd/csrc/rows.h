@@ -38,10 +38,21 @@ __device__ __forceinline__ u32x4_t narrow(const float* f) {
     return v;
 }
 
+// Sum over the 64 lanes, the same in each: six adds on the vector unit with lanes
+// moved within rows of 16 (row_shr 1, 2, 4, 8), then from row to row (row_bcast 15
+// and 31), without the LDS that a shuffle goes through.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float add_moved(float v) {
+    return v + bit_cast<float>(__builtin_amdgcn_update_dpp(0, bit_cast<int>(v), CTRL, ROWS, 0xF, true));
+}
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
+    v = add_moved<0x111, 0xF>(v);
+    v = add_moved<0x112, 0xF>(v);
+    v = add_moved<0x114, 0xF>(v);
+    v = add_moved<0x118, 0xF>(v);
+    v = add_moved<0x142, 0xA>(v);
+    v = add_moved<0x143, 0xC>(v);
+    return bit_cast<float>(__builtin_amdgcn_readlane(bit_cast<int>(v), 63));
 }
 
 // ---- 8-bit checkpoints ------------------------------------------------------
