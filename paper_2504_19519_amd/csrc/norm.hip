@@ -29,119 +29,147 @@
 namespace fo {
 namespace {
 
-// Sums of `v` over the TH threads of a row (TH > 64: the whole workgroup; `lds`
-// has TH / 64 words that nothing else uses until the next barrier).
-template <int TH>
-__device__ __forceinline__ float row_sum(float v, float* lds) {
-    v = wave_sum(v);
-    if constexpr (TH > 64) {
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = 0.0f;
-#pragma unroll
-        for (int w = 0; w < TH / 64; ++w) v += lds[w];
-    }
-    return v;
-}
-
+// ROWS rows at a time, TH threads each. Every thread keeps its columns of gamma and
+// beta, and the next row's loads are issued ahead of this row's sums. Where a row
+// has several waves each takes the mean of its own values and the sum of their
+// squared differences from it, and one meeting joins them:
+//   sum of (x - mu)^2 = sum over waves of (their sum + n_w (mu_w - mu)^2).
 template <int DT, int CH, int TH, int ROWS>
 __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs a) {
-    static_assert(TH == 64 || ROWS == 1, "a barrier per row");
-    __shared__ float s_mean[TH / 64], s_square[TH / 64];
-    const int lane = threadIdx.x % TH;
-    const int64_t i = (int64_t)blockIdx.x * ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / TH);
-    if (i >= a.M) return;
-    const uint16_t* row = a.x + i * a.ldx;
+    constexpr int kRowWaves = TH / 64;
+    __shared__ float s_sum[2][2][TH * ROWS / 64];
+    // (a wave lies within one row: its row is the same for every lane)
+    const int lane = threadIdx.x % TH, group = __builtin_amdgcn_readfirstlane(threadIdx.x / TH);
     const int full = (int)(a.N >> 3), tail = (int)(a.N & 7);
+    const bool has_tail = lane < tail;
+    const int64_t blocks = (a.N + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK, step = (int64_t)gridDim.x * ROWS;
     // A lane's sum is scaled by the power of two that makes N at most 1, so that the
     // row's sums (of squares: up to 2^120 on average) stay in fp32's range.
-    const float n = (float)a.N * a.scale;
+    const float scale = a.scale, n = (float)a.N * scale;
 
-    u32x4_t v[CH];
+    u32x4_t gamma[CH], beta[CH];
+    float gamma_t = 1.0f, beta_t = 0.0f, count = has_tail ? 1.0f : 0.0f;
 #pragma unroll
     for (int t = 0; t < CH; ++t) {
         const int c = lane + TH * t;
-        v[t] = u32x4_t{0u, 0u, 0u, 0u};
-        if (c < full) v[t] = load8(row + 8 * c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            gamma[t][e] = pack2<DT>(1.0f, 1.0f);
+            beta[t][e] = 0u;
+        }
+        if (c < full) {
+            if (a.gamma) gamma[t] = load8(a.gamma + 8 * c);
+            if (a.beta) beta[t] = load8(a.beta + 8 * c);
+            count += 8.0f;
+        }
     }
-    const bool has_tail = lane < tail;
-    const float xt = has_tail ? to_f32<DT>(row[8 * full + lane]) : 0.0f;
+    if (a.gamma && has_tail) gamma_t = to_f32<DT>(a.gamma[8 * full + lane]);
+    if (a.beta && has_tail) beta_t = to_f32<DT>(a.beta[8 * full + lane]);
+    count = wave_sum(count * scale);                // of this wave, scaled like the sums
+    float wave_count = 0.0f;                        // lane w: of the row's wave w
+    if constexpr (kRowWaves > 1) {
+        if ((threadIdx.x & 63) == 0) s_sum[0][0][threadIdx.x >> 6] = count;
+        __syncthreads();
+        if ((threadIdx.x & 63) < kRowWaves) wave_count = s_sum[0][0][group * kRowWaves + (threadIdx.x & 63)];
+        __syncthreads();
+    }
 
-    if (a.packed) {
-        const int64_t blocks = (a.N + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK;
-        uint8_t* packed = a.packed + i * blocks * FO_PACK_BLOCK;
-        uint8_t* scales = a.scales + i * blocks;
-        const int whole = (int)(a.N / FO_PACK_BLOCK) * 4;
+    auto load = [&](int64_t i, u32x4_t* v, uint32_t& vt) {
+        const uint16_t* row = a.x + i * a.ldx;
 #pragma unroll
         for (int t = 0; t < CH; ++t) {
             const int c = lane + TH * t;
-            if (c < whole) {
-                if (a.format == FO_PACK_INT8) pack_chunk<DT, FO_PACK_INT8>(v[t], c, packed, scales);
-                else pack_chunk<DT, FO_PACK_E4M3>(v[t], c, packed, scales);
+            v[t] = u32x4_t{0u, 0u, 0u, 0u};
+            if (i < a.M && c < full) v[t] = load8(row + 8 * c);
+        }
+        vt = i < a.M && has_tail ? row[8 * full + lane] : 0u;
+    };
+
+    int64_t i = (int64_t)blockIdx.x * ROWS + group;
+    const int64_t rounds = (a.M - (int64_t)blockIdx.x * ROWS + step - 1) / step;   // the same for every row group
+    u32x4_t next[CH];
+    uint32_t next_t;
+    load(i, next, next_t);
+    for (int64_t round = 0; round < rounds; ++round, i += step) {
+        u32x4_t v[CH];
+#pragma unroll
+        for (int t = 0; t < CH; ++t) v[t] = next[t];
+        const float xt = to_f32<DT>(next_t);
+        if (round + 1 < rounds) load(i + step, next, next_t);
+
+        if (a.packed && i < a.M) {
+            uint8_t* packed = a.packed + i * blocks * FO_PACK_BLOCK;
+            uint8_t* scales = a.scales + i * blocks;
+            const int whole = (int)(a.N / FO_PACK_BLOCK) * 4;
+#pragma unroll
+            for (int t = 0; t < CH; ++t) {
+                const int c = lane + TH * t;
+                if (c < whole) {
+                    if (a.format == FO_PACK_INT8) pack_chunk<DT, FO_PACK_INT8>(v[t], c, packed, scales);
+                    else pack_chunk<DT, FO_PACK_E4M3>(v[t], c, packed, scales);
+                }
+            }
+            // (read again here, ahead of any store to y, which may be x)
+            if (a.N % FO_PACK_BLOCK && lane < 64) {
+                const uint16_t* row = a.x + i * a.ldx;
+                if (a.format == FO_PACK_INT8) pack_last<DT, FO_PACK_INT8>(row, a.N, lane, packed, scales);
+                else pack_last<DT, FO_PACK_E4M3>(row, a.N, lane, packed, scales);
             }
         }
-        // (read again here, ahead of any store to y, which may be x)
-        if (a.N % FO_PACK_BLOCK && lane < 64) {
-            if (a.format == FO_PACK_INT8) pack_last<DT, FO_PACK_INT8>(row, a.N, lane, packed, scales);
-            else pack_last<DT, FO_PACK_E4M3>(row, a.N, lane, packed, scales);
-        }
-    }
 
-    float mean = 0.0f;
-    if (a.layer) {
-        float sum = xt;
+        float x[CH][8], sum = 0.0f, mean = 0.0f, square = 0.0f;
 #pragma unroll
         for (int t = 0; t < CH; ++t) {
-            float f[8];
-            widen<DT>(v[t], f);
+            widen<DT>(v[t], x[t]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += f[e];
+            for (int e = 0; e < 8; ++e) sum += x[t][e];
         }
-        mean = row_sum<TH>(sum * a.scale, s_mean) / n;
-    }
-    float square = has_tail ? (xt - mean) * (xt - mean) : 0.0f;
+        if (tail) sum += xt;
+        // the wave's own mean (an RMS norm: differences from zero)
+        sum = wave_sum(sum * scale);
+        if (a.layer && count > 0.0f) mean = sum / count;
 #pragma unroll
-    for (int t = 0; t < CH; ++t) {
-        float f[8], q = 0.0f;
-        widen<DT>(v[t], f);
+        for (int t = 0; t < CH; ++t) {
+            float q = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) q += (f[e] - mean) * (f[e] - mean);
-        if (lane + TH * t < full) square += q;
-    }
-    const float rstd = 1.0f / sqrtf(row_sum<TH>(square * a.scale, s_square) / n + a.eps);
-    if (lane == 0) {
-        if (a.mean) a.mean[i] = mean;
-        if (a.rstd) a.rstd[i] = rstd;
-    }
-
-    uint16_t* out = a.y + i * a.ldy;
-#pragma unroll
-    for (int t = 0; t < CH; ++t) {
-        const int c = lane + TH * t;
-        if (c < full) {
-            float f[8], p[8];
-            widen<DT>(v[t], f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = (f[e] - mean) * rstd;
-            if (a.gamma) {
-                widen<DT>(load8(a.gamma + 8 * c), p);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] *= p[e];
-            }
-            if (a.beta) {
-                widen<DT>(load8(a.beta + 8 * c), p);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] += p[e];
-            }
-            store8(out + 8 * c, narrow<DT>(f));
+            for (int e = 0; e < 8; ++e) q += (x[t][e] - mean) * (x[t][e] - mean);
+            if (lane + TH * t < full) square += q;
         }
-    }
-    if (has_tail) {
-        const int c = 8 * full + lane;
-        float f = (xt - mean) * rstd;
-        if (a.gamma) f *= to_f32<DT>(a.gamma[c]);
-        if (a.beta) f += to_f32<DT>(a.beta[c]);
-        out[c] = (uint16_t)from_f32<DT>(f);
+        if (has_tail) square += (xt - mean) * (xt - mean);
+        square = wave_sum(square * scale);
+        if constexpr (kRowWaves > 1) {
+            // (two sets of words, so that one barrier per row is enough)
+            const int set = (int)(round & 1), wave = threadIdx.x >> 6, w = threadIdx.x & 63;
+            if (w == 0) {
+                s_sum[set][0][wave] = mean;
+                s_sum[set][1][wave] = square;
+            }
+            __syncthreads();
+            const bool there = w < kRowWaves;
+            const float mw = there ? s_sum[set][0][group * kRowWaves + w] : 0.0f;
+            const float qw = there ? s_sum[set][1][group * kRowWaves + w] : 0.0f;
+            mean = a.layer ? wave_sum(mw * wave_count) / n : 0.0f;
+            square = wave_sum(qw + wave_count * ((mw - mean) * (mw - mean)));
+        }
+        const float rstd = 1.0f / sqrtf(square / n + a.eps);
+        if (i >= a.M) continue;
+        if (lane == 0) {
+            if (a.mean) a.mean[i] = mean;
+            if (a.rstd) a.rstd[i] = rstd;
+        }
+        uint16_t* out = a.y + i * a.ldy;
+#pragma unroll
+        for (int t = 0; t < CH; ++t) {
+            const int c = lane + TH * t;
+            float g[8], b[8];
+            asm volatile("" : "+v"(gamma[t]), "+v"(beta[t]));      // widened anew for each row: half the registers
+            widen<DT>(gamma[t], g);
+            widen<DT>(beta[t], b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] = (x[t][e] - mean) * rstd * g[e] + b[e];
+            if (c < full) stream8(out + 8 * c, narrow<DT>(g));
+        }
+        if (has_tail) out[8 * full + lane] = (uint16_t)from_f32<DT>((xt - mean) * rstd * gamma_t + beta_t);
     }
 }
 
@@ -291,7 +319,7 @@ __global__ __launch_bounds__(TH * ROWS) void norm_backward_kernel(const NormArgs
                 float d[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) d[e] = rstd * gv[t][e] - c1 - tv[t][e] * c2;
-                if (c < full) store8(out + 8 * c, narrow<DT>(d));
+                if (c < full) stream8(out + 8 * c, narrow<DT>(d));
             }
             if (has_tail) out[8 * full + lane] = (uint16_t)from_f32<DT>(rstd * gt - c1 - tt * c2);
         }
@@ -378,25 +406,7 @@ __global__ __launch_bounds__(kReduceThreads) void norm_reduce_kernel(const float
 template <int N>
 using Int = std::integral_constant<int, N>;
 
-// The forward form's constants, as go(chunks, threads, rows).
-template <typename F>
-void for_forward(const NormForm& f, F go) {
-    if (f.threads == 64) {
-        if (f.chunks == 1) go(Int<1>(), Int<64>(), Int<4>());
-        else if (f.chunks == 2) go(Int<2>(), Int<64>(), Int<4>());
-        else go(Int<4>(), Int<64>(), Int<4>());
-    } else if (f.threads == 256) {
-        if (f.chunks == 2) go(Int<2>(), Int<256>(), Int<1>());
-        else go(Int<4>(), Int<256>(), Int<1>());
-    } else if (f.threads == 512) {
-        go(Int<4>(), Int<512>(), Int<1>());
-    } else {
-        go(Int<4>(), Int<1024>(), Int<1>());
-    }
-}
-
-// The same for the backward pass: two chunks per thread, and as many rows at a time
-// as the rows give every compute unit.
+// A form's constants, as go(chunks, threads, rows).
 template <int TH, typename F>
 void for_rows(const NormForm& f, F go) {
     if constexpr (TH <= 64) {
@@ -414,7 +424,7 @@ void for_rows(const NormForm& f, F go) {
     go(Int<2>(), Int<TH>(), Int<1>());
 }
 template <typename F>
-void for_backward(const NormForm& f, F go) {
+void for_form(const NormForm& f, F go) {
     if (f.threads == 64) for_rows<64>(f, go);
     else if (f.threads == 128) for_rows<128>(f, go);
     else if (f.threads == 256) for_rows<256>(f, go);
@@ -425,30 +435,30 @@ void for_backward(const NormForm& f, F go) {
 
 }  // namespace
 
-NormForm norm_forward_form(int64_t M, int64_t N) {
-    NormForm f{};
-    f.threads = N <= 2048 ? 64 : N <= 8192 ? 256 : N <= 16384 ? 512 : 1024;
-    const int64_t per = (N / 8 + f.threads - 1) / f.threads;
-    f.chunks = per <= 1 && f.threads == 64 ? 1 : per <= 2 && f.threads <= 256 ? 2 : 4;
-    f.rows = f.threads == 64 ? 4 : 1;
-    f.blocks = (uint32_t)((M + f.rows - 1) / f.rows);
-    return f;
-}
-
-NormForm norm_backward_form(int64_t M, int64_t N) {
-    constexpr int kUnits = 256;            // compute units of an MI355X
+// Two chunks of a row per thread (four past 16384 columns), and in a workgroup of up
+// to `threads` as many rows at a time as leave every one of `units` workgroups some.
+static NormForm row_form(int64_t M, int64_t N, int threads, int64_t units) {
     NormForm f{};
     f.threads = N <= 1024 ? 64 : N <= 2048 ? 128 : N <= 4096 ? 256 : N <= 8192 ? 512 : 1024;
     f.chunks = N <= 16384 ? 2 : 4;
     f.rows = 1;
-    while (f.rows * 2 * f.threads <= 1024 && f.rows * 2 * (int64_t)kUnits <= M) f.rows *= 2;
-    f.blocks = (uint32_t)std::min<int64_t>((M + f.rows - 1) / f.rows, kUnits);
+    while (f.rows * 2 * f.threads <= threads && f.rows * 2 * units <= M) f.rows *= 2;
+    f.blocks = (uint32_t)std::min<int64_t>((M + f.rows - 1) / f.rows, units);
     return f;
 }
 
+// Forward: three workgroups of eight waves per compute unit (8192x8192 fp16 54 us,
+// 16384x4096 bf16 with a checkpoint 58; one of 16 waves, on more rows, 66 for the
+// second; registers held down to two of 16 waves 69 and 83; a workgroup per row and
+// nothing ahead 60 and 61). Past 8192 columns, where a row has 16 waves and they fit
+// once: one (1280x12288 20.1; 22.8 with three, two of them waiting).
+NormForm norm_forward_form(int64_t M, int64_t N) { return row_form(M, N, 512, N <= 8192 ? 768 : 256); }
+// Backward: one of 16 waves, whose registers leave no more.
+NormForm norm_backward_form(int64_t M, int64_t N) { return row_form(M, N, 1024, 256); }
+
 hipError_t launch_norm_forward(int dtype, const NormArgs& a, hipStream_t s) {
     const NormForm f = norm_forward_form(a.M, a.N);
-    for_forward(f, [&](auto ch, auto th, auto rows) {
+    for_form(f, [&](auto ch, auto th, auto rows) {
         constexpr int CH = decltype(ch)::value, TH = decltype(th)::value, ROWS = decltype(rows)::value;
         const dim3 g(f.blocks), b(TH * ROWS);
         if (dtype == FO_FP16) hipLaunchKernelGGL((norm_forward_kernel<FO_FP16, CH, TH, ROWS>), g, b, 0, s, a);
@@ -460,7 +470,7 @@ hipError_t launch_norm_forward(int dtype, const NormArgs& a, hipStream_t s) {
 hipError_t launch_norm_backward(int dtype, const NormArgs& a, float* dgamma, float* dbeta, hipStream_t s) {
     const NormForm f = norm_backward_form(a.M, a.N);
     if (a.M > 0) {
-        for_backward(f, [&](auto ch, auto th, auto rows) {
+        for_form(f, [&](auto ch, auto th, auto rows) {
             constexpr int CH = decltype(ch)::value, TH = decltype(th)::value, ROWS = decltype(rows)::value;
             const dim3 g(f.blocks), b(TH * ROWS);
             auto go = [&](auto dt, auto src) {

@@ -105,10 +105,8 @@ fo_status fo_norm_forward(int32_t kind, int32_t dtype, int64_t M, int64_t N, con
         (st = fo::check_vectors(gamma, beta, mean, rstd)) != FO_OK ||
         ((packed || scales) && (st = fo::check_pack(packed, scales, format)) != FO_OK))
         return st;
+    if (M > INT32_MAX) return fo::fail(FO_ERR_SHAPE, "2^31 rows or more");
     if (fo::clash(x, ldx, y, ldy, M, N, true)) return fo::fail(FO_ERR_ARG, "y overlaps x without being x");
-    const fo::NormForm f = fo::norm_forward_form(M, N);
-    if (!fo::launchable((M + f.rows - 1) / f.rows, f.threads * f.rows))
-        return fo::fail(FO_ERR_SHAPE, "too many rows for one launch");
     fo::NormArgs a{};
     a.x = static_cast<const uint16_t*>(x);
     a.gamma = static_cast<const uint16_t*>(gamma);
@@ -145,6 +143,7 @@ fo_status fo_norm_backward(int32_t kind, int32_t dtype, int64_t M, int64_t N, co
     if (!fo::aligned(dgamma, 4) || !fo::aligned(dbeta, 4))
         return fo::fail(FO_ERR_ARG, "dgamma and dbeta must be 4-byte aligned");
     if (N == 0) return FO_OK;
+    if (M > INT32_MAX) return fo::fail(FO_ERR_SHAPE, "2^31 rows or more");
     const bool sums = dgamma || dbeta;
     if (M > 0) {
         if (!x == !(packed || scales)) return fo::fail(FO_ERR_ARG, "x or a checkpoint of it, one of the two");

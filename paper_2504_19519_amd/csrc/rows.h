@@ -20,6 +20,12 @@ __device__ __forceinline__ u32x4_t load8(const uint16_t* p) {
     return v;
 }
 __device__ __forceinline__ void store8(uint16_t* p, u32x4_t v) { __builtin_memcpy(p, &v, sizeof(v)); }
+// The same past the caches' keeping (nontemporal): large outputs that this kernel
+// does not read again.
+typedef uint32_t u32x4_near_t __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ void stream8(uint16_t* p, u32x4_t v) {
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4_near_t*>(p));
+}
 
 template <int DT>
 __device__ __forceinline__ void widen(u32x4_t v, float* f) {
@@ -163,9 +169,10 @@ __device__ __forceinline__ void decode8(u32x2_t code, float scale, float* f) {
 template <int DT, int FMT>
 __device__ __forceinline__ void pack_chunk(u32x4_t v, int c, uint8_t* packed_row, uint8_t* scale_row) {
     uint32_t top = top_bits(v);
-    uint32_t other = __shfl_xor(top, 1, 64);
+    // the other three lanes': quad_perm [1, 0, 3, 2], then [2, 3, 0, 1]
+    uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, true);
     top = top > other ? top : other;
-    other = __shfl_xor(top, 2, 64);
+    other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xF, 0xF, true);
     top = top > other ? top : other;
     const BlockScale b = block_scale<DT, FMT>(top);
     float f[8];
