@@ -12,7 +12,10 @@
 // Permute, combine and the combine's backward pass move whole rows of H values
 // and are bound by memory: each row is read once (a token's row stays in
 // registers while it goes to its K places, a token's K rows are in flight
-// together).
+// together). They write past the caches (nontemporal), which leaves these to what
+// is read: 16384 tokens to 8 of 128 experts, H 2048, 115 -> 103 us; 4096 tokens from
+// 8 experts, H 7168, 104 -> 95; 4096 tokens, 2 experts, combine with a checkpoint and
+// its backward pass in turn, 53 + 42 -> 43 + 44.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -25,7 +28,8 @@ namespace fo {
 namespace {
 
 constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64;
-constexpr int64_t kSortRun = 8192;          // pairs of one workgroup, at least
+constexpr int64_t kSortAlone = 8192;        // pairs that one workgroup sorts by itself
+constexpr int64_t kSortRun = 2048;          // pairs of one workgroup among several, at least
 constexpr int kSortBlocks = 256;            // workgroups, at most
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 
@@ -53,7 +57,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs
 template <typename ID>
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs a, int64_t run) {
     __shared__ int32_t s_place[kSortWaves][kMaxExperts];
-    __shared__ int32_t s_first[kMaxExperts], s_total[kMaxExperts], s_wave[kSortWaves];
+    __shared__ int32_t s_first[kMaxExperts + 1], s_total[kMaxExperts], s_before[kMaxExperts], s_wave[kSortWaves];
     const ID* ids = static_cast<const ID*>(a.ids);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, E = a.experts;
     const int64_t first = blockIdx.x * run, end = first + run < a.pairs ? first + run : a.pairs;
@@ -67,23 +71,36 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
         if (e >= 0) atomicAdd(&s_place[wave][e], 1);
     }
     __syncthreads();
-    // per expert: the parts' counts to their first places within the expert
-    for (int e = threadIdx.x; e < E; e += kSortThreads) {
-        int32_t before = 0, total = 0;
-        if (gridDim.x > 1) {
-            for (uint32_t b = 0; b < gridDim.x; ++b) {
+    // all workgroups' counts and those ahead of this one: kSortThreads / E threads per
+    // expert, each over its share of the workgroups
+    for (int e = threadIdx.x; e < E; e += kSortThreads) s_total[e] = s_before[e] = 0;
+    __syncthreads();
+    if (gridDim.x > 1) {
+        const int shares = E < kSortThreads ? kSortThreads / E : 1;
+        const int share = E < kSortThreads ? (int)threadIdx.x / E : 0;
+        for (int e = threadIdx.x - share * E; share < shares && e < E; e += kSortThreads) {
+            int32_t before = 0, total = 0;
+#pragma unroll 8
+            for (int b = share; b < (int)gridDim.x; b += shares) {
                 const int32_t n = a.hist[(int64_t)b * E + e];
-                before += b < blockIdx.x ? n : 0;
+                before += b < (int)blockIdx.x ? n : 0;
                 total += n;
             }
+            atomicAdd(&s_total[e], total);
+            atomicAdd(&s_before[e], before);
         }
+        __syncthreads();
+    }
+    // per expert: the parts' counts to their first places within the expert
+    for (int e = threadIdx.x; e < E; e += kSortThreads) {
+        const int32_t before = s_before[e];
         int32_t at = before;
         for (int w = 0; w < kSortWaves; ++w) {
             const int32_t n = s_place[w][e];
             s_place[w][e] = at;
             at += n;
         }
-        s_total[e] = gridDim.x > 1 ? total : at;
+        if (gridDim.x == 1) s_total[e] = at;
     }
     __syncthreads();
     // the experts' first rows: two experts per thread, padded counts summed up
@@ -93,7 +110,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
         for (int j = 0; j < 2; ++j) {
             const int e = 2 * threadIdx.x + j;
             mine[j] = sum;
-            if (e < E) sum += (int32_t)(((int64_t)s_total[e] + a.align - 1) / a.align * a.align);
+            if (e < E) sum += (int32_t)(((uint32_t)s_total[e] + (uint32_t)a.align - 1) / (uint32_t)a.align * (uint32_t)a.align);
         }
         int32_t scan = sum;
 #pragma unroll
@@ -109,6 +126,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
         for (int j = 0; j < 2; ++j) {
             const int e = 2 * threadIdx.x + j;
             if (e < E) s_first[e] = base + mine[j];
+            if (e == E - 1) s_first[E] = base + sum;
             if (blockIdx.x == 0) {
                 if (e < E) {
                     a.offsets[e] = base + mine[j];
@@ -119,13 +137,10 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
         }
     }
     __syncthreads();
-    // padding rows belong to no pair
-    if (a.pair_of) {
-        for (int e = blockIdx.x; e < E; e += gridDim.x) {
-            const int32_t from = s_first[e] + s_total[e];
-            const int32_t to = s_first[e] + (int32_t)(((int64_t)s_total[e] + a.align - 1) / a.align * a.align);
-            for (int32_t r = from + threadIdx.x; r < to; r += kSortThreads) a.pair_of[r] = -1;
-        }
+    // padding rows belong to no pair: a wave per expert
+    if (a.pair_of && a.align > 1) {
+        for (int e = blockIdx.x * kSortWaves + wave; e < E; e += gridDim.x * kSortWaves)
+            for (int32_t r = s_first[e] + s_total[e] + lane; r < s_first[e + 1]; r += 64) a.pair_of[r] = -1;
     }
     int bits = 0;
     while ((1 << bits) < E) ++bits;
@@ -176,7 +191,7 @@ __device__ __forceinline__ void zero_padding(const RouteArgs& a, uint16_t* rows,
     const int full = (int)(a.H >> 3), tail = (int)(a.H & 7);
     for (int64_t r = (int64_t)from + wave; r < to; r += per * kWaves) {
         uint16_t* row = rows + r * ld;
-        for (int c = lane; c < full; c += 64) store8(row + 8 * (int64_t)c, u32x4_t{0u, 0u, 0u, 0u});
+        for (int c = lane; c < full; c += 64) stream8(row + 8 * (int64_t)c, u32x4_t{0u, 0u, 0u, 0u});
         if (lane < tail) row[8 * (int64_t)full + lane] = 0;
     }
 }
@@ -198,7 +213,7 @@ __global__ __launch_bounds__(kThreads) void permute_kernel(const RouteArgs a, ui
         const int32_t slot = a.slot_of[(int64_t)u.t * a.K + k];
         if (!is_row(a, slot)) continue;
         uint16_t* out = a.rows + slot * a.ldr;
-        if (c < full) store8(out + 8 * (int64_t)c, v);
+        if (c < full) stream8(out + 8 * (int64_t)c, v);
         if (has_tail) out[8 * (int64_t)full + lane] = vt;
     }
 }
@@ -233,7 +248,7 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(const RouteArgs a, ui
         }
     }
     uint16_t* out = a.out + u.t * a.ldo;
-    if (c < full) store8(out + 8 * (int64_t)c, narrow<DT>(sum));
+    if (c < full) stream8(out + 8 * (int64_t)c, narrow<DT>(sum));
     if (has_tail) out[8 * (int64_t)full + lane] = (uint16_t)from_f32<DT>(sum_t);
 }
 
@@ -271,7 +286,7 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const RouteA
         if (out) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) g[e] *= w;
-            store8(out + 8 * (int64_t)c, narrow<DT>(g));
+            stream8(out + 8 * (int64_t)c, narrow<DT>(g));
         }
     }
     if (lane < tail) {
@@ -299,7 +314,7 @@ using Int = std::integral_constant<int, N>;
 }  // namespace
 
 int64_t sort_blocks(int64_t pairs) {
-    return std::max<int64_t>(1, std::min<int64_t>((pairs + kSortRun - 1) / kSortRun, kSortBlocks));
+    return pairs <= kSortAlone ? 1 : std::min<int64_t>((pairs + kSortRun - 1) / kSortRun, kSortBlocks);
 }
 
 hipError_t launch_sort(const SortArgs& a, hipStream_t s) {
