@@ -586,30 +586,44 @@ def _pick(table, key, what: str) -> int:
         raise ValueError(f"{what}: one of {[k for k in table if isinstance(k, str)]}, got {key!r}") from None
 
 
+_TYPES = {}          # element types that an argument takes, once a tensor has been seen
+
+
+def _types(kind):
+    """Torch dtypes of a kind of argument: the values' (FP16, BF16: that type or a 16-bit
+    container), "f32", "i32", "ids", "u8"."""
+    if not _TYPES:
+        t = sys.modules["torch"]
+        bits = {t.int16, t.uint16}
+        _TYPES.update({FP16: {t.float16} | bits, BF16: {t.bfloat16} | bits, "f32": {t.float32},
+                       "i32": {t.int32, t.uint32}, "ids": {t.int32, t.int64}, "u8": {t.uint8, t.int8}})
+    return _TYPES[kind]
+
+
 class _Args:
     """Pointers of one row operator's arguments. Tensors are checked: on one GPU,
-    the current one (and the stream's), of the element size and dtype that the call
-    takes, large enough, and contiguous or (matrices) with rows of unit stride. Raw
-    pointers are taken as given."""
+    the current one (and the stream's), of the dtype that the call takes, large
+    enough, and contiguous or (matrices) with rows of unit stride. Raw pointers are
+    taken as given."""
 
     __slots__ = ("dtype", "device")
 
     def __init__(self, dtype, stream):
         self.dtype = _pick(_DTYPES, dtype, "dtype")
-        self.device = getattr(stream, "device_index", None)
-        if self.device is None:
-            torch = sys.modules.get("torch")
-            if torch is not None and torch.cuda.is_initialized():
-                self.device = torch.cuda.current_device()
+        self.device = None
+        torch = sys.modules.get("torch")
+        if torch is not None and torch.cuda.is_initialized():
+            self.device = torch.cuda.current_device()
+            at = getattr(stream, "device_index", self.device)
+            if at != self.device:
+                raise ValueError(f"stream: of device {at}, the current one is {self.device}")
 
-    def _on_device(self, x, what):
-        d = x.get_device()
+    def _other_device(self, d, what):
         if d < 0:
             raise ValueError(f"{what}: a tensor on the GPU is needed")
-        if self.device is None:
-            self.device = d
-        elif d != self.device:
+        if self.device is not None:
             raise ValueError(f"{what}: on device {d}, the call runs on device {self.device}")
+        self.device = d
 
     def rows(self, x, M: int, N: int, ld, what: str):
         """(pointer, row distance) of a [M, N] matrix of 16-bit values."""
@@ -617,36 +631,37 @@ class _Args:
             return None, N
         if not hasattr(x, "get_device"):
             return _ptr(x), N if ld is None else int(ld)
-        self._on_device(x, what)
-        if x.element_size() != 2 or self._other(x):
+        d = x.get_device()
+        if d != self.device:
+            self._other_device(d, what)
+        if x.dtype not in _types(self.dtype):
             raise ValueError(f"{what}: {x.dtype} values for {'bf16' if self.dtype else 'fp16'}")
-        if ld is None and x.dim() == 2 and x.shape[1] == N:
-            if x.shape[0] < M:
-                raise ValueError(f"{what}: {x.shape[0]} rows, the call needs {M}")
-            step, unit = x.stride()
-            if (unit != 1 and N > 1) or (step < N and M > 1):
-                raise ValueError(f"{what}: rows of unit stride that do not overlap are needed, strides are "
-                                 f"{tuple(x.stride())}")
-            return x.data_ptr(), step if M > 1 else N
+        if ld is None and x.dim() == 2:
+            have, length = x.shape
+            if length == N:
+                if have < M:
+                    raise ValueError(f"{what}: {have} rows, the call needs {M}")
+                step, unit = x.stride()
+                if (unit != 1 and N > 1) or (step < N and M > 1):
+                    raise ValueError(f"{what}: rows of unit stride that do not overlap are needed, strides are "
+                                     f"{tuple(x.stride())}")
+                return x.data_ptr(), step if M > 1 else N
         ld = N if ld is None else int(ld)
         need = (M - 1) * ld + N if M > 0 and N > 0 else 0
         if not x.is_contiguous() or x.numel() < need:
             raise ValueError(f"{what}: {need} contiguous elements are needed, or a [{M}, {N}] view")
         return x.data_ptr(), ld
 
-    def _other(self, x) -> bool:
-        """Whether x holds the other 16-bit floating type (integer containers fit both)."""
-        return x.is_floating_point() and (str(x.dtype) == "torch.bfloat16") != (self.dtype == BF16)
-
-    def flat(self, x, count: int, what: str, size: int = 4, floating=None):
-        """Pointer of `count` contiguous elements of `size` bytes."""
+    def flat(self, x, count: int, what: str, kind=None):
+        """Pointer of `count` contiguous elements of a kind (None: the values')."""
         if x is None:
             return None
         if not hasattr(x, "get_device"):
             return _ptr(x)
-        self._on_device(x, what)
-        if x.element_size() != size or (floating is not None and x.is_floating_point() != floating) or (
-                size == 2 and self._other(x)):
+        d = x.get_device()
+        if d != self.device:
+            self._other_device(d, what)
+        if x.dtype not in _types(self.dtype if kind is None else kind):
             raise ValueError(f"{what}: elements of {x.dtype}")
         if not x.is_contiguous() or x.numel() < count:
             raise ValueError(f"{what}: {count} contiguous elements are needed")
@@ -658,7 +673,9 @@ class _Args:
             return None, 0
         if not hasattr(x, "get_device"):
             return _ptr(x), (1 << 63) - 1
-        self._on_device(x, what)
+        d = x.get_device()
+        if d != self.device:
+            self._other_device(d, what)
         if not x.is_contiguous():
             raise ValueError(f"{what}: contiguous memory is needed")
         return x.data_ptr(), x.numel() * x.element_size()
@@ -668,7 +685,7 @@ class _Args:
         if packed is None and scales is None:
             return None, None, 0
         codes, steps = packed_bytes(M, N)
-        return (self.flat(packed, codes, "packed", 1, False), self.flat(scales, steps, "scales", 1, False),
+        return (self.flat(packed, codes, "packed", "u8"), self.flat(scales, steps, "scales", "u8"),
                 _pick(_FORMATS, fmt, "fmt"))
 
 
@@ -692,9 +709,9 @@ def norm_forward(kind, x, gamma, beta, y, M: int, N: int, dtype, eps: float = 1e
     px, sx = a.rows(x, M, N, ldx, "x")
     py, sy = a.rows(y, M, N, ldy, "y")
     codes, steps, fmt = a.pack(packed, scales, M, N, fmt)
-    _check(lib().fo_norm_forward(_pick(_NORMS, kind, "kind"), a.dtype, M, N, px, sx, a.flat(gamma, N, "gamma", 2),
-                                 a.flat(beta, N, "beta", 2), eps, py, sy, a.flat(mean, M, "mean", 4, True),
-                                 a.flat(rstd, M, "rstd", 4, True), codes, steps, fmt, _stream(stream)))
+    _check(lib().fo_norm_forward(_pick(_NORMS, kind, "kind"), a.dtype, M, N, px, sx, a.flat(gamma, N, "gamma"),
+                                 a.flat(beta, N, "beta"), eps, py, sy, a.flat(mean, M, "mean", "f32"),
+                                 a.flat(rstd, M, "rstd", "f32"), codes, steps, fmt, _stream(stream)))
 
 
 def norm_backward(kind, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, M: int, N: int, dtype, workspace=None,
@@ -708,9 +725,9 @@ def norm_backward(kind, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, M: int, N: 
     codes, steps, fmt = a.pack(packed, scales, M, N, fmt)
     work, size = a.space(workspace)
     _check(lib().fo_norm_backward(_pick(_NORMS, kind, "kind"), a.dtype, M, N, pg, sg, px, sx, codes, steps, fmt,
-                                  a.flat(gamma, N, "gamma", 2), a.flat(mean, M, "mean", 4, True),
-                                  a.flat(rstd, M, "rstd", 4, True), pd, sd, a.flat(dgamma, N, "dgamma", 4, True),
-                                  a.flat(dbeta, N, "dbeta", 4, True), work, size, _stream(stream)))
+                                  a.flat(gamma, N, "gamma"), a.flat(mean, M, "mean", "f32"),
+                                  a.flat(rstd, M, "rstd", "f32"), pd, sd, a.flat(dgamma, N, "dgamma", "f32"),
+                                  a.flat(dbeta, N, "dbeta", "f32"), work, size, _stream(stream)))
 
 
 def pack_rows(x, packed, scales, M: int, N: int, dtype, fmt="int8", ldx=None, stream=None) -> None:
@@ -750,9 +767,9 @@ def route_sort(ids, T: int, K: int, E: int, offsets, counts, slot_of, pair_of=No
     rows = int(capacity) if capacity is not None else pair_of.numel() if hasattr(pair_of, "numel") else \
         route_capacity(T, K, E, align)
     work, nbytes = a.space(workspace)
-    _check(lib().fo_route_sort(a.flat(ids, T * K, "ids", size, False), size, T, K, E, align,
-                               a.flat(offsets, E + 1, "offsets", 4, False), a.flat(counts, E, "counts", 4, False),
-                               a.flat(slot_of, T * K, "slot_of", 4, False), a.flat(pair_of, rows, "pair_of", 4, False),
+    _check(lib().fo_route_sort(a.flat(ids, T * K, "ids", "ids"), size, T, K, E, align,
+                               a.flat(offsets, E + 1, "offsets", "i32"), a.flat(counts, E, "counts", "i32"),
+                               a.flat(slot_of, T * K, "slot_of", "i32"), a.flat(pair_of, rows, "pair_of", "i32"),
                                rows, work, nbytes, _stream(stream)))
 
 
@@ -763,9 +780,9 @@ def route_permute(x, slot_of, rows, T: int, K: int, H: int, dtype, capacity: int
     a = _Args(dtype, stream)
     px, sx = a.rows(x, T, H, ldx, "x")
     pr, sr = a.rows(rows, capacity, H, ldr, "rows")
-    _check(lib().fo_route_permute(a.dtype, T, K, H, px, sx, a.flat(slot_of, T * K, "slot_of", 4, False), pr, sr,
-                                  capacity, a.flat(offsets, E + 1, "offsets", 4, False),
-                                  a.flat(counts, E, "counts", 4, False), E, _stream(stream)))
+    _check(lib().fo_route_permute(a.dtype, T, K, H, px, sx, a.flat(slot_of, T * K, "slot_of", "i32"), pr, sr,
+                                  capacity, a.flat(offsets, E + 1, "offsets", "i32"),
+                                  a.flat(counts, E, "counts", "i32"), E, _stream(stream)))
 
 
 def route_combine(rows, slot_of, weights, out, T: int, K: int, H: int, dtype, capacity: int, packed=None, scales=None,
@@ -777,8 +794,8 @@ def route_combine(rows, slot_of, weights, out, T: int, K: int, H: int, dtype, ca
     pr, sr = a.rows(rows, capacity, H, ldr, "rows")
     po, so = a.rows(out, T, H, ldo, "out")
     codes, steps, fmt = a.pack(packed, scales, capacity, H, fmt)
-    _check(lib().fo_route_combine(a.dtype, T, K, H, pr, sr, capacity, a.flat(slot_of, T * K, "slot_of", 4, False),
-                                  a.flat(weights, T * K, "weights", 4, True), po, so, codes, steps, fmt,
+    _check(lib().fo_route_combine(a.dtype, T, K, H, pr, sr, capacity, a.flat(slot_of, T * K, "slot_of", "i32"),
+                                  a.flat(weights, T * K, "weights", "f32"), po, so, codes, steps, fmt,
                                   _stream(stream)))
 
 
@@ -794,8 +811,8 @@ def route_combine_backward(dout, rows, slot_of, weights, drows, dweights, T: int
     pd, sd = a.rows(drows, capacity, H, lddr, "drows")
     codes, steps, fmt = a.pack(packed, scales, capacity, H, fmt)
     _check(lib().fo_route_combine_backward(a.dtype, T, K, H, pg, sg, pr, sr, codes, steps, fmt, capacity,
-                                           a.flat(slot_of, T * K, "slot_of", 4, False),
-                                           a.flat(weights, T * K, "weights", 4, True), pd, sd,
-                                           a.flat(dweights, T * K, "dweights", 4, True),
-                                           a.flat(offsets, E + 1, "offsets", 4, False),
-                                           a.flat(counts, E, "counts", 4, False), E, _stream(stream)))
+                                           a.flat(slot_of, T * K, "slot_of", "i32"),
+                                           a.flat(weights, T * K, "weights", "f32"), pd, sd,
+                                           a.flat(dweights, T * K, "dweights", "f32"),
+                                           a.flat(offsets, E + 1, "offsets", "i32"),
+                                           a.flat(counts, E, "counts", "i32"), E, _stream(stream)))
