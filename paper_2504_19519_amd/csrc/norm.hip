@@ -45,7 +45,13 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
     const int64_t blocks = (a.N + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK, step = (int64_t)gridDim.x * ROWS;
     // A lane's sum is scaled by the power of two that makes N at most 1, so that the
     // row's sums (of squares: up to 2^120 on average) stay in fp32's range.
-    const float scale = a.scale, n = (float)a.N * scale;
+    const float scale = a.scale, n = (float)a.N * scale, inv_n = 1.0f / n;
+    // A sum's quotient by n: the error of the product with 1 / n is taken back, so that a
+    // row of one value has that value for its mean.
+    auto mean_of = [&](float sum) {
+        const float q = sum * inv_n;
+        return q + (sum - q * n) * inv_n;
+    };
 
     u32x4_t gamma[CH], beta[CH];
     float gamma_t = 1.0f, beta_t = 0.0f, count = has_tail ? 1.0f : 0.0f;
@@ -66,6 +72,7 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
     if (a.gamma && has_tail) gamma_t = to_f32<DT>(a.gamma[8 * full + lane]);
     if (a.beta && has_tail) beta_t = to_f32<DT>(a.beta[8 * full + lane]);
     count = wave_sum(count * scale);                // of this wave, scaled like the sums
+    const float inv_count = count > 0.0f ? 1.0f / count : 0.0f;
     float wave_count = 0.0f;                        // lane w: of the row's wave w
     if constexpr (kRowWaves > 1) {
         if ((threadIdx.x & 63) == 0) s_sum[0][0][threadIdx.x >> 6] = count;
@@ -91,9 +98,9 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
     uint32_t next_t;
     load(i, next, next_t);
     for (int64_t round = 0; round < rounds; ++round, i += step) {
-        u32x4_t v[CH];
+        float x[CH][8];
 #pragma unroll
-        for (int t = 0; t < CH; ++t) v[t] = next[t];
+        for (int t = 0; t < CH; ++t) widen<DT>(next[t], x[t]);
         const float xt = to_f32<DT>(next_t);
         if (round + 1 < rounds) load(i + step, next, next_t);
 
@@ -105,8 +112,8 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
             for (int t = 0; t < CH; ++t) {
                 const int c = lane + TH * t;
                 if (c < whole) {
-                    if (a.format == FO_PACK_INT8) pack_chunk<DT, FO_PACK_INT8>(v[t], c, packed, scales);
-                    else pack_chunk<DT, FO_PACK_E4M3>(v[t], c, packed, scales);
+                    if (a.format == FO_PACK_INT8) pack_chunk<DT, FO_PACK_INT8>(x[t], c, packed, scales);
+                    else pack_chunk<DT, FO_PACK_E4M3>(x[t], c, packed, scales);
                 }
             }
             // (read again here, ahead of any store to y, which may be x)
@@ -117,17 +124,16 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
             }
         }
 
-        float x[CH][8], sum = 0.0f, mean = 0.0f, square = 0.0f;
+        float mean = 0.0f, square = 0.0f;
+        if (a.layer) {          // (an RMS norm: differences from zero)
+            float sum = xt;
 #pragma unroll
-        for (int t = 0; t < CH; ++t) {
-            widen<DT>(v[t], x[t]);
+            for (int t = 0; t < CH; ++t)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += x[t][e];
+                for (int e = 0; e < 8; ++e) sum += x[t][e];
+            sum = wave_sum(sum * scale);
+            mean = kRowWaves > 1 ? sum * inv_count : mean_of(sum);
         }
-        if (tail) sum += xt;
-        // the wave's own mean (an RMS norm: differences from zero)
-        sum = wave_sum(sum * scale);
-        if (a.layer && count > 0.0f) mean = sum / count;
 #pragma unroll
         for (int t = 0; t < CH; ++t) {
             float q = 0.0f;
@@ -148,10 +154,10 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
             const bool there = w < kRowWaves;
             const float mw = there ? s_sum[set][0][group * kRowWaves + w] : 0.0f;
             const float qw = there ? s_sum[set][1][group * kRowWaves + w] : 0.0f;
-            mean = a.layer ? wave_sum(mw * wave_count) / n : 0.0f;
-            square = wave_sum(qw + wave_count * ((mw - mean) * (mw - mean)));
+            mean = a.layer ? mean_of(first_sum<kRowWaves>(mw * wave_count)) : 0.0f;
+            square = first_sum<kRowWaves>(qw + wave_count * ((mw - mean) * (mw - mean)));
         }
-        const float rstd = 1.0f / sqrtf(square / n + a.eps);
+        const float rstd = rsqrt_of(square * inv_n + a.eps);
         if (i >= a.M) continue;
         if (lane == 0) {
             if (a.mean) a.mean[i] = mean;
@@ -295,8 +301,7 @@ __global__ __launch_bounds__(TH * ROWS) void norm_backward_kernel(const NormArgs
             s2 += gt * tt;
         }
         load(i + step, next);
-        s1 = wave_sum(s1);
-        s2 = wave_sum(s2);
+        wave_sums(s1, s2);
         if constexpr (kRowWaves > 1) {
             // (two sets of words, so that one barrier per row is enough)
             const int set = (int)(n & 1), wave = threadIdx.x >> 6;
@@ -306,8 +311,8 @@ __global__ __launch_bounds__(TH * ROWS) void norm_backward_kernel(const NormArgs
             }
             __syncthreads();
             const int w = threadIdx.x & 63;
-            s1 = wave_sum(w < kRowWaves ? s_sum[set][0][group * kRowWaves + w] : 0.0f);
-            s2 = wave_sum(w < kRowWaves ? s_sum[set][1][group * kRowWaves + w] : 0.0f);
+            s1 = first_sum<kRowWaves>(w < kRowWaves ? s_sum[set][0][group * kRowWaves + w] : 0.0f);
+            s2 = first_sum<kRowWaves>(w < kRowWaves ? s_sum[set][1][group * kRowWaves + w] : 0.0f);
         }
         if (a.dx && i < a.M) {
             const float c1 = a.layer ? rstd * (s1 * inv_n) : 0.0f;

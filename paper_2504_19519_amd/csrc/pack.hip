@@ -22,7 +22,11 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const PackArgs a, uint32
     uint8_t* packed = a.packed + i * blocks * FO_PACK_BLOCK;
     uint8_t* scales = a.scales + i * blocks;
     const int c = (int)s * 64 + lane;
-    if (c < a.N / FO_PACK_BLOCK * 4) pack_chunk<DT, FMT>(load8(row + 8 * (int64_t)c), c, packed, scales);
+    if (c < a.N / FO_PACK_BLOCK * 4) {
+        float f[8];
+        widen<DT>(load8(row + 8 * (int64_t)c), f);
+        pack_chunk<DT, FMT>(f, c, packed, scales);
+    }
     if (s == slices - 1 && a.N % FO_PACK_BLOCK) pack_last<DT, FMT>(row, a.N, lane, packed, scales);
 }
 

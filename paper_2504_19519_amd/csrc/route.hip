@@ -243,7 +243,7 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(const RouteArgs a, ui
             const int64_t blocks = (a.H + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK;
             uint8_t* packed = a.packed + slot * blocks * FO_PACK_BLOCK;
             uint8_t* scales = a.scales + slot * blocks;
-            if (c < a.H / FO_PACK_BLOCK * 4) pack_chunk<DT, FMT>(v, c, packed, scales);
+            if (c < a.H / FO_PACK_BLOCK * 4) pack_chunk<DT, FMT>(f, c, packed, scales);
             if (u.s == (int)slices - 1 && a.H % FO_PACK_BLOCK) pack_last<DT, FMT>(row, a.H, lane, packed, scales);
         }
     }

@@ -61,6 +61,38 @@ __device__ __forceinline__ float wave_sum(float v) {
     return bit_cast<float>(__builtin_amdgcn_readlane(bit_cast<int>(v), 63));
 }
 
+// Two sums over the 64 lanes for little more than one: the halves change places, so
+// that the lower lanes go on with a's sum and the upper ones with b's.
+__device__ __forceinline__ void wave_sums(float& a, float& b) {
+    const u32x2_t swapped = bit_cast<u32x2_t>(
+        __builtin_amdgcn_permlane32_swap(bit_cast<uint32_t>(a), bit_cast<uint32_t>(b), false, false));
+    float v = bit_cast<float>(swapped[0]) + bit_cast<float>(swapped[1]);
+    v = add_moved<0x111, 0xF>(v);
+    v = add_moved<0x112, 0xF>(v);
+    v = add_moved<0x114, 0xF>(v);
+    v = add_moved<0x118, 0xF>(v);
+    v = add_moved<0x142, 0xA>(v);
+    a = bit_cast<float>(__builtin_amdgcn_readlane(bit_cast<int>(v), 31));
+    b = bit_cast<float>(__builtin_amdgcn_readlane(bit_cast<int>(v), 63));
+}
+// Sum over the first W lanes (a power of two up to 16), the same in each lane.
+template <int W>
+__device__ __forceinline__ float first_sum(float v) {
+    if constexpr (W > 1) v = add_moved<0x111, 0xF>(v);
+    if constexpr (W > 2) v = add_moved<0x112, 0xF>(v);
+    if constexpr (W > 4) v = add_moved<0x114, 0xF>(v);
+    if constexpr (W > 8) v = add_moved<0x118, 0xF>(v);
+    return bit_cast<float>(__builtin_amdgcn_readlane(bit_cast<int>(v), W - 1));
+}
+
+// 1 / sqrt(v), within 1.5 steps of fp32: the hardware's, which takes values below the
+// normal range as zero, for a scaled value where v may be one.
+__device__ __forceinline__ float rsqrt_of(float v) {
+    const bool small = v < 0x1p-96f;
+    const float r = __builtin_amdgcn_rsqf(small ? v * 0x1p64f : v);
+    return small ? r * 0x1p32f : r;
+}
+
 // ---- 8-bit checkpoints ------------------------------------------------------
 // A block of 32 values shares a scale 2^s, stored as s + 127; value = code * 2^s.
 // With 2^e the largest power of two <= the block's largest magnitude:
@@ -70,16 +102,15 @@ __device__ __forceinline__ float wave_sum(float v) {
 // s >= -126, so that 2^s and 2^-s are normal fp32 numbers and the products exact: the
 // only rounding is the code's. A block with an infinity or a NaN has scale byte 255
 // (2^s reads as infinity) and codes 0, which read as NaN.
-// Eight lanes' worth of a block: four lanes of one chunk each.
 
-typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2_t __attribute__((ext_vector_type(2)));
 
-// Largest magnitude bits of eight values.
-__device__ __forceinline__ uint32_t top_bits(u32x4_t v) {
-    u16x2_t m = bit_cast<u16x2_t>(v[0] & 0x7FFF7FFFu);
+// Largest magnitude of eight values, NaN if one is.
+__device__ __forceinline__ float top_of(const float* f) {
+    float m = __builtin_elementwise_maximum(__builtin_fabsf(f[0]), __builtin_fabsf(f[1]));
 #pragma unroll
-    for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, bit_cast<u16x2_t>(v[i] & 0x7FFF7FFFu));
-    return m[0] > m[1] ? m[0] : m[1];
+    for (int e = 2; e < 8; ++e) m = __builtin_elementwise_maximum(m, __builtin_fabsf(f[e]));
+    return m;
 }
 
 struct BlockScale {
@@ -88,10 +119,10 @@ struct BlockScale {
     uint32_t byte;              // s + 127, or 255
 };
 
-// The scale of a block from the bits of its largest magnitude.
+// The scale of a block from its largest magnitude.
 template <int DT, int FMT>
-__device__ __forceinline__ BlockScale block_scale(uint32_t top) {
-    const uint32_t bits = bit_cast<uint32_t>(to_f32<DT>(top));
+__device__ __forceinline__ BlockScale block_scale(float top) {
+    const uint32_t bits = bit_cast<uint32_t>(top) & 0x7FFFFFFFu;
     int s;
     BlockScale b;
     if constexpr (FMT == FO_PACK_INT8) {
@@ -104,8 +135,7 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t top) {
         b.limit = e > (DT == FO_FP16 ? 15 : 127) ? 240.0f : 448.0f;
     }
     s = s < -126 ? -126 : s;
-    const bool finite = top < (DT == FO_FP16 ? 0x7C00u : 0x7F80u);
-    b.byte = finite ? (uint32_t)(s + 127) : 255u;
+    b.byte = bits < 0x7F800000u ? (uint32_t)(s + 127) : 255u;
     b.inverse = bit_cast<float>((uint32_t)(127 - s) << 23);
     return b;
 }
@@ -113,18 +143,25 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t top) {
 // Four values' codes, little-endian.
 template <int FMT>
 __device__ __forceinline__ uint32_t encode4(const float* f, const BlockScale& b) {
-    float v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_fmed3f(f[i] * b.inverse, -b.limit, b.limit);
     uint32_t code;
     if constexpr (FMT == FO_PACK_INT8) {
-        // v + 1.5 * 2^23 rounds v to a whole number (to nearest even), whose low byte
-        // is the code
-        uint32_t w[4];
+        // x / 2^s + 1.5 * 2^23 rounds x / 2^s to a whole number (to nearest even), which
+        // its low 16 bits hold; two of them at a time are kept within [-127, 127]
+        uint32_t w[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = bit_cast<uint32_t>(v[i] + 12582912.0f) & 0xFFu;
-        code = w[0] | (w[1] << 8) | (w[2] << 16) | (w[3] << 24);
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t lo = bit_cast<uint32_t>(__builtin_fmaf(f[2 * i], b.inverse, 12582912.0f));
+            const uint32_t hi = bit_cast<uint32_t>(__builtin_fmaf(f[2 * i + 1], b.inverse, 12582912.0f));
+            i16x2_t v = bit_cast<i16x2_t>(__builtin_amdgcn_perm(hi, lo, 0x05040100u));
+            v = __builtin_elementwise_min(v, i16x2_t{127, 127});
+            v = __builtin_elementwise_max(v, i16x2_t{-127, -127});
+            w[i] = bit_cast<uint32_t>(v);
+        }
+        code = __builtin_amdgcn_perm(w[1], w[0], 0x06040200u);
     } else {
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_fmed3f(f[i] * b.inverse, -b.limit, b.limit);
         int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
         w = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], w, true);
         code = (uint32_t)w;
@@ -164,19 +201,17 @@ __device__ __forceinline__ void decode8(u32x2_t code, float scale, float* f) {
     decode4<FMT>(code[1], scale, f + 4);
 }
 
-// A lane's chunk of a whole block, packed with the three neighbours' that share it
-// (lanes 4 i .. 4 i + 3 hold chunks 4 j .. 4 j + 3; every lane of the four calls).
+// A lane's chunk f of a whole block, packed with the three neighbours' that share it
+// (lanes 4 i .. 4 i + 3 hold chunks 4 j .. 4 j + 3; all four lanes call).
 template <int DT, int FMT>
-__device__ __forceinline__ void pack_chunk(u32x4_t v, int c, uint8_t* packed_row, uint8_t* scale_row) {
-    uint32_t top = top_bits(v);
+__device__ __forceinline__ void pack_chunk(const float* f, int c, uint8_t* packed_row, uint8_t* scale_row) {
+    float top = top_of(f);
     // the other three lanes': quad_perm [1, 0, 3, 2], then [2, 3, 0, 1]
-    uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, true);
-    top = top > other ? top : other;
-    other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xF, 0xF, true);
-    top = top > other ? top : other;
+    top = __builtin_elementwise_maximum(
+        top, bit_cast<float>(__builtin_amdgcn_update_dpp(0, bit_cast<int>(top), 0xB1, 0xF, 0xF, true)));
+    top = __builtin_elementwise_maximum(
+        top, bit_cast<float>(__builtin_amdgcn_update_dpp(0, bit_cast<int>(top), 0x4E, 0xF, 0xF, true)));
     const BlockScale b = block_scale<DT, FMT>(top);
-    float f[8];
-    widen<DT>(v, f);
     u32x2_t code;
     code[0] = encode4<FMT>(f, b);
     code[1] = encode4<FMT>(f + 4, b);
@@ -191,12 +226,9 @@ __device__ __forceinline__ void pack_last(const uint16_t* row, int64_t N, int la
                                           uint8_t* scale_row) {
     const int64_t block = N / FO_PACK_BLOCK, n = block * FO_PACK_BLOCK + lane;
     const uint32_t bits = lane < FO_PACK_BLOCK && n < N ? row[n] : 0u;
-    uint32_t top = bits & 0x7FFFu;
+    float top = __builtin_fabsf(to_f32<DT>(bits));
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        const uint32_t other = __shfl_xor(top, off, 64);
-        top = top > other ? top : other;
-    }
+    for (int off = 16; off > 0; off >>= 1) top = __builtin_elementwise_maximum(top, __shfl_xor(top, off, 64));
     if (lane < FO_PACK_BLOCK) {
         const BlockScale b = block_scale<DT, FMT>(top);
         const float f[4] = {to_f32<DT>(bits), 0.0f, 0.0f, 0.0f};
