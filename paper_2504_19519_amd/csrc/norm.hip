@@ -196,7 +196,7 @@ struct RowPart {
 // and of the two sums over rows; with the next row's loads issued ahead of this
 // row's sums, one workgroup of 16 waves per compute unit keeps memory busy, and
 // there are few workgroups' sums to add.
-template <int DT, int SRC, int CH, int TH, int ROWS>
+template <int DT, int SRC, int CH, int TH, int ROWS, int AHEAD>
 __global__ __launch_bounds__(TH * ROWS) void norm_backward_kernel(const NormArgs a) {
     constexpr int kWaves = TH * ROWS / 64, kRowWaves = TH / 64;
     __shared__ float s_sum[2][2][kWaves];
@@ -263,9 +263,11 @@ __global__ __launch_bounds__(TH * ROWS) void norm_backward_kernel(const NormArgs
 
     int64_t i = (int64_t)blockIdx.x * ROWS + group;
     const int64_t rounds = (a.M - (int64_t)blockIdx.x * ROWS + step - 1) / step;   // the same for every row group
-    RowPart<SRC, CH> next;
-    load(i, next);
-    for (int64_t n = 0; n < rounds; ++n, i += step) {
+    RowPart<SRC, CH> ahead[AHEAD];
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d) load(i + d * step, ahead[d]);
+    // one round: the row i whose loads `next` holds, which then takes those of row i + AHEAD * step
+    auto round = [&](int64_t n, RowPart<SRC, CH>& next) {
         // With t = x - mean: h = t rstd, so that
         //   dgamma += (dy rstd) t,  sum(g h) = rstd sum(g t),
         //   dx = rstd g - rstd mean(g) - t rstd^2 mean(g h).
@@ -300,7 +302,7 @@ __global__ __launch_bounds__(TH * ROWS) void norm_backward_kernel(const NormArgs
             s1 += gt;
             s2 += gt * tt;
         }
-        load(i + step, next);
+        load(i + AHEAD * step, next);
         wave_sums(s1, s2);
         if constexpr (kRowWaves > 1) {
             // (two sets of words, so that one barrier per row is enough)
@@ -328,6 +330,12 @@ __global__ __launch_bounds__(TH * ROWS) void norm_backward_kernel(const NormArgs
             }
             if (has_tail) out[8 * full + lane] = (uint16_t)from_f32<DT>(rstd * gt - c1 - tt * c2);
         }
+        i += step;
+    };
+    for (int64_t n = 0; n < rounds; n += AHEAD) {
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d)
+            if (n + d < rounds) round(n + d, ahead[d]);
     }
     if (!a.partial) return;
     // The row groups' sums, added in halves: group g takes group g + h's.
@@ -412,58 +420,73 @@ template <int N>
 using Int = std::integral_constant<int, N>;
 
 // A form's constants, as go(chunks, threads, rows).
-template <int TH, typename F>
+template <int CH, int TH, int MAX, typename F>
 void for_rows(const NormForm& f, F go) {
-    if constexpr (TH <= 64) {
-        if (f.rows == 16) return go(Int<2>(), Int<TH>(), Int<16>());
+    if constexpr (MAX > 1) {
+        if (f.rows < MAX) return for_rows<CH, TH, MAX / 2>(f, go);
     }
-    if constexpr (TH <= 128) {
-        if (f.rows == 8) return go(Int<2>(), Int<TH>(), Int<8>());
-    }
-    if constexpr (TH <= 256) {
-        if (f.rows == 4) return go(Int<2>(), Int<TH>(), Int<4>());
-    }
-    if constexpr (TH <= 512) {
-        if (f.rows == 2) return go(Int<2>(), Int<TH>(), Int<2>());
-    }
-    go(Int<2>(), Int<TH>(), Int<1>());
+    go(Int<CH>(), Int<TH>(), Int<MAX>());
 }
 template <typename F>
-void for_form(const NormForm& f, F go) {
-    if (f.threads == 64) for_rows<64>(f, go);
-    else if (f.threads == 128) for_rows<128>(f, go);
-    else if (f.threads == 256) for_rows<256>(f, go);
-    else if (f.threads == 512) for_rows<512>(f, go);
-    else if (f.chunks == 2) for_rows<1024>(f, go);
-    else go(Int<4>(), Int<1024>(), Int<1>());
+void for_forward(const NormForm& f, F go) {
+    if (f.threads == 64) for_rows<2, 64, 8>(f, go);
+    else if (f.threads == 128) for_rows<2, 128, 4>(f, go);
+    else if (f.threads == 256) for_rows<2, 256, 2>(f, go);
+    else if (f.threads == 512) for_rows<2, 512, 1>(f, go);
+    else if (f.chunks == 2) for_rows<2, 1024, 1>(f, go);
+    else for_rows<4, 1024, 1>(f, go);
+}
+template <typename F>
+void for_backward(const NormForm& f, F go) {
+    if (f.threads == 64) for_rows<1, 64, 16>(f, go);
+    else if (f.threads == 128) for_rows<1, 128, 8>(f, go);
+    else if (f.threads == 256) for_rows<1, 256, 4>(f, go);
+    else if (f.threads == 512) for_rows<1, 512, 2>(f, go);
+    else if (f.threads == 768) for_rows<2, 768, 1>(f, go);
+    else if (f.chunks == 1) for_rows<1, 1024, 1>(f, go);
+    else if (f.chunks == 2) for_rows<2, 1024, 1>(f, go);
+    else for_rows<4, 1024, 1>(f, go);
 }
 
-}  // namespace
-
-// Two chunks of a row per thread (four past 16384 columns), and in a workgroup of up
-// to `threads` as many rows at a time as leave every one of `units` workgroups some.
-static NormForm row_form(int64_t M, int64_t N, int threads, int64_t units) {
-    NormForm f{};
-    f.threads = N <= 1024 ? 64 : N <= 2048 ? 128 : N <= 4096 ? 256 : N <= 8192 ? 512 : 1024;
-    f.chunks = N <= 16384 ? 2 : 4;
+// As many rows at a time, in a workgroup of up to `threads`, as leave every one of
+// `units` workgroups some.
+void set_rows(NormForm& f, int64_t M, int threads, int64_t units) {
     f.rows = 1;
     while (f.rows * 2 * f.threads <= threads && f.rows * 2 * units <= M) f.rows *= 2;
     f.blocks = (uint32_t)std::min<int64_t>((M + f.rows - 1) / f.rows, units);
-    return f;
 }
+
+}  // namespace
 
 // Forward: three workgroups of eight waves per compute unit (8192x8192 fp16 54 us,
 // 16384x4096 bf16 with a checkpoint 58; one of 16 waves, on more rows, 66 for the
 // second; registers held down to two of 16 waves 69 and 83; a workgroup per row and
 // nothing ahead 60 and 61). Past 8192 columns, where a row has 16 waves and they fit
 // once: one (1280x12288 20.1; 22.8 with three, two of them waiting).
-NormForm norm_forward_form(int64_t M, int64_t N) { return row_form(M, N, 512, N <= 8192 ? 768 : 256); }
-// Backward: one of 16 waves, whose registers leave no more.
-NormForm norm_backward_form(int64_t M, int64_t N) { return row_form(M, N, 1024, 256); }
+NormForm norm_forward_form(int64_t M, int64_t N) {
+    NormForm f{};
+    f.threads = N <= 1024 ? 64 : N <= 2048 ? 128 : N <= 4096 ? 256 : N <= 8192 ? 512 : 1024;
+    f.chunks = N <= 16384 ? 2 : 4;
+    set_rows(f, M, 512, N <= 8192 ? 768 : 256);
+    return f;
+}
+
+// Backward: one workgroup of 16 waves per compute unit. One chunk of a row per thread
+// while 16 waves take a row so: its registers leave room for the loads of three rows
+// ahead (16384x4096 bf16 from an int8 checkpoint 57 us, one row ahead 63, four 58; two
+// chunks and one row ahead 66, two rows ahead do not fit and take 140).
+NormForm norm_backward_form(int64_t M, int64_t N) {
+    NormForm f{};
+    f.threads = N <= 512 ? 64 : N <= 1024 ? 128 : N <= 2048 ? 256 : N <= 4096 ? 512 : N <= 8192 ? 1024
+              : N <= 12288 ? 768 : 1024;
+    f.chunks = N <= 8192 ? 1 : N <= 16384 ? 2 : 4;
+    set_rows(f, M, 1024, 256);
+    return f;
+}
 
 hipError_t launch_norm_forward(int dtype, const NormArgs& a, hipStream_t s) {
     const NormForm f = norm_forward_form(a.M, a.N);
-    for_form(f, [&](auto ch, auto th, auto rows) {
+    for_forward(f, [&](auto ch, auto th, auto rows) {
         constexpr int CH = decltype(ch)::value, TH = decltype(th)::value, ROWS = decltype(rows)::value;
         const dim3 g(f.blocks), b(TH * ROWS);
         if (dtype == FO_FP16) hipLaunchKernelGGL((norm_forward_kernel<FO_FP16, CH, TH, ROWS>), g, b, 0, s, a);
@@ -475,11 +498,13 @@ hipError_t launch_norm_forward(int dtype, const NormArgs& a, hipStream_t s) {
 hipError_t launch_norm_backward(int dtype, const NormArgs& a, float* dgamma, float* dbeta, hipStream_t s) {
     const NormForm f = norm_backward_form(a.M, a.N);
     if (a.M > 0) {
-        for_form(f, [&](auto ch, auto th, auto rows) {
+        for_backward(f, [&](auto ch, auto th, auto rows) {
             constexpr int CH = decltype(ch)::value, TH = decltype(th)::value, ROWS = decltype(rows)::value;
+            // rows ahead, as the registers of the workgroup's waves allow
+            constexpr int AHEAD = CH == 1 ? 3 : TH == 768 ? 2 : 1;
             const dim3 g(f.blocks), b(TH * ROWS);
             auto go = [&](auto dt, auto src) {
-                hipLaunchKernelGGL((norm_backward_kernel<decltype(dt)::value, decltype(src)::value, CH, TH, ROWS>), g, b,
+                hipLaunchKernelGGL((norm_backward_kernel<decltype(dt)::value, decltype(src)::value, CH, TH, ROWS, AHEAD>), g, b,
                                    0, s, a);
             };
             const int src = a.packed ? 1 + a.format : 0;
