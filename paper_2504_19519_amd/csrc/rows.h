@@ -26,6 +26,10 @@ typedef uint32_t u32x4_near_t __attribute__((ext_vector_type(4), aligned(2)));
 __device__ __forceinline__ void stream8(uint16_t* p, u32x4_t v) {
     __builtin_nontemporal_store(v, reinterpret_cast<u32x4_near_t*>(p));
 }
+// And inputs that are read once.
+__device__ __forceinline__ u32x4_t stream_load8(const uint16_t* p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4_near_t*>(p));
+}
 
 template <int DT>
 __device__ __forceinline__ void widen(u32x4_t v, float* f) {
