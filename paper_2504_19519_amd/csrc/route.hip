@@ -15,7 +15,8 @@
 // together). They write past the caches (nontemporal), which leaves these to what
 // is read: 16384 tokens to 8 of 128 experts, H 2048, 115 -> 103 us; 4096 tokens from
 // 8 experts, H 7168, 104 -> 95; 4096 tokens, 2 experts, combine with a checkpoint and
-// its backward pass in turn, 53 + 42 -> 43 + 44.
+// its backward pass in turn, 53 + 42 -> 43 + 44. With the combine's rows loaded past
+// the caches too, four of a token's at a time: 90 us (5.9 TB/s), and 42 + 43.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -32,6 +33,7 @@ constexpr int64_t kSortAlone = 8192;        // pairs that one workgroup sorts by
 constexpr int64_t kSortRun = 2048;          // pairs of one workgroup among several, at least
 constexpr int kSortBlocks = 256;            // workgroups, at most
 constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kBatch = 4;                   // rows of a token in flight
 
 template <typename ID>
 __device__ __forceinline__ int expert_of(const ID* ids, int64_t p, int64_t end, int experts) {
@@ -184,12 +186,13 @@ __device__ __forceinline__ Unit unit_of(uint32_t slices) {
 // workgroups per expert, a wave per row at a time.
 __device__ __forceinline__ void zero_padding(const RouteArgs& a, uint16_t* rows, int64_t ld, uint32_t block, int per) {
     const int e = (int)(block / (uint32_t)per), lane = threadIdx.x & 63;
-    const int wave = (int)(block % (uint32_t)per) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int waves = blockDim.x >> 6;
+    const int wave = (int)(block % (uint32_t)per) * waves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int32_t from = a.offsets[e] + a.counts[e], to = a.offsets[e + 1];
     from = from < 0 ? 0 : from;
     to = to > a.capacity ? a.capacity : to;
     const int full = (int)(a.H >> 3), tail = (int)(a.H & 7);
-    for (int64_t r = (int64_t)from + wave; r < to; r += per * kWaves) {
+    for (int64_t r = (int64_t)from + wave; r < to; r += per * waves) {
         uint16_t* row = rows + r * ld;
         for (int c = lane; c < full; c += 64) stream8(row + 8 * (int64_t)c, u32x4_t{0u, 0u, 0u, 0u});
         if (lane < tail) row[8 * (int64_t)full + lane] = 0;
@@ -218,33 +221,51 @@ __global__ __launch_bounds__(kThreads) void permute_kernel(const RouteArgs a, ui
     }
 }
 
-// FMT: -1, or the format of the checkpoint that the rows are packed into.
+// FMT: -1, or the format of the checkpoint that the rows are packed into. kBatch of
+// a token's rows are in flight together.
 template <int DT, int FMT>
 __global__ __launch_bounds__(kThreads) void combine_kernel(const RouteArgs a, uint32_t slices) {
     const Unit u = unit_of(slices);
     if (u.t >= a.T) return;
     const int lane = threadIdx.x & 63, full = (int)(a.H >> 3), tail = (int)(a.H & 7), c = u.s * 64 + lane;
-    const bool has_tail = u.s == (int)slices - 1 && lane < tail;
+    const bool last = u.s == (int)slices - 1, has_tail = last && lane < tail;
+    const int64_t blocks = (a.H + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK, first = (int64_t)u.t * a.K;
     float sum[8] = {}, sum_t = 0.0f;
-    for (int k = 0; k < a.K; ++k) {
-        const int64_t p = (int64_t)u.t * a.K + k;
-        const int32_t slot = a.slot_of[p];
-        if (!is_row(a, slot)) continue;
-        const float w = a.weights ? a.weights[p] : 1.0f;
-        const uint16_t* row = a.rows + slot * a.ldr;
-        u32x4_t v{};
-        if (c < full) v = load8(row + 8 * (int64_t)c);
-        float f[8];
-        widen<DT>(v, f);
+    for (int k0 = 0; k0 < a.K; k0 += kBatch) {
+        int32_t slot[kBatch];
+        float w[kBatch];
+        u32x4_t v[kBatch];
+        uint32_t vt[kBatch];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] += w * f[e];
-        if (has_tail) sum_t += w * to_f32<DT>(row[8 * (int64_t)full + lane]);
-        if constexpr (FMT >= 0) {
-            const int64_t blocks = (a.H + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK;
-            uint8_t* packed = a.packed + slot * blocks * FO_PACK_BLOCK;
-            uint8_t* scales = a.scales + slot * blocks;
-            if (c < a.H / FO_PACK_BLOCK * 4) pack_chunk<DT, FMT>(f, c, packed, scales);
-            if (u.s == (int)slices - 1 && a.H % FO_PACK_BLOCK) pack_last<DT, FMT>(row, a.H, lane, packed, scales);
+        for (int j = 0; j < kBatch; ++j) {
+            slot[j] = k0 + j < a.K ? a.slot_of[first + k0 + j] : -1;
+            w[j] = k0 + j < a.K && a.weights ? a.weights[first + k0 + j] : 1.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            v[j] = u32x4_t{0u, 0u, 0u, 0u};
+            vt[j] = 0u;
+            if (is_row(a, slot[j])) {
+                const uint16_t* row = a.rows + slot[j] * a.ldr;
+                if (c < full) v[j] = stream_load8(row + 8 * (int64_t)c);
+                if (has_tail) vt[j] = row[8 * (int64_t)full + lane];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            if (!is_row(a, slot[j])) continue;
+            float f[8];
+            widen<DT>(v[j], f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += w[j] * f[e];
+            sum_t += w[j] * to_f32<DT>(vt[j]);
+            if constexpr (FMT >= 0) {
+                uint8_t* packed = a.packed + slot[j] * blocks * FO_PACK_BLOCK;
+                uint8_t* scales = a.scales + slot[j] * blocks;
+                if (c < a.H / FO_PACK_BLOCK * 4) pack_chunk<DT, FMT>(f, c, packed, scales);
+                if (last && a.H % FO_PACK_BLOCK)
+                    pack_last<DT, FMT>(a.rows + slot[j] * a.ldr, a.H, lane, packed, scales);
+            }
         }
     }
     uint16_t* out = a.out + u.t * a.ldo;
@@ -252,14 +273,19 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(const RouteArgs a, ui
     if (has_tail) out[8 * (int64_t)full + lane] = (uint16_t)from_f32<DT>(sum_t);
 }
 
-// A wave per pair: drows[slot] = w dout[t] and dw = <dout[t], rows[slot]>. SRC: where
-// the rows come from: 0 themselves, 1 + format a checkpoint of them.
-template <int DT, int SRC>
+// WAVES waves per pair, each along its row: drows[slot] = w dout[t] and dw =
+// <dout[t], rows[slot]>. SRC: where the rows come from: 0 themselves, 1 + format a
+// checkpoint of them.
+template <int DT, int SRC, int WAVES>
 __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const RouteArgs a, uint32_t blocks, int per) {
+    static_assert(WAVES == 1 || WAVES == kWaves, "a workgroup's pair meets once");
+    constexpr int kLanes = 64 * WAVES;
+    __shared__ float s_dot[kWaves];
     if (blockIdx.x >= blocks) return zero_padding(a, a.out, a.ldo, blockIdx.x - blocks, per);
-    const int64_t p = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t p = (int64_t)blockIdx.x * (kWaves / WAVES) + wave / WAVES;
     if (p >= (int64_t)a.T * a.K) return;
-    const int lane = threadIdx.x & 63, full = (int)(a.H >> 3), tail = (int)(a.H & 7);
+    const int lane = threadIdx.x % kLanes, full = (int)(a.H >> 3), tail = (int)(a.H & 7);
     const int32_t slot = a.slot_of[p];
     if (!is_row(a, slot)) {
         if (lane == 0 && a.dweights) a.dweights[p] = 0.0f;
@@ -267,18 +293,18 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const RouteA
     }
     const float w = a.weights ? a.weights[p] : 1.0f;
     const int64_t blocks32 = (a.H + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK;
-    const uint16_t* grow = a.x + p / a.K * a.ldx;
+    const uint16_t* grow = a.x + (uint32_t)p / (uint32_t)a.K * a.ldx;
     const uint16_t* row = SRC == 0 && a.dweights ? a.rows + slot * a.ldr : nullptr;
     const uint8_t* packed = SRC ? a.packed + slot * blocks32 * FO_PACK_BLOCK : nullptr;
     const uint8_t* scales = SRC ? a.scales + slot * blocks32 : nullptr;
     uint16_t* out = a.out ? a.out + slot * a.ldo : nullptr;
     float dot = 0.0f;
-    for (int c = lane; c < full; c += 64) {
+    for (int c = lane; c < full; c += kLanes) {
         float g[8];
         widen<DT>(load8(grow + 8 * (int64_t)c), g);
         if (a.dweights) {
             float f[8];
-            if constexpr (SRC == 0) widen<DT>(load8(row + 8 * (int64_t)c), f);
+            if constexpr (SRC == 0) widen<DT>(stream_load8(row + 8 * (int64_t)c), f);
             else decode8<SRC - 1>(*reinterpret_cast<const u32x2_t*>(packed + 8 * (int64_t)c), scale_of(scales[c >> 2]), f);
 #pragma unroll
             for (int e = 0; e < 8; ++e) dot += g[e] * f[e];
@@ -300,6 +326,13 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const RouteA
     }
     if (a.dweights) {
         dot = wave_sum(dot);
+        if constexpr (WAVES > 1) {
+            if ((threadIdx.x & 63) == 0) s_dot[wave] = dot;
+            __syncthreads();
+            dot = 0.0f;
+#pragma unroll
+            for (int v = 0; v < WAVES; ++v) dot += s_dot[v];
+        }
         if (lane == 0) a.dweights[p] = dot;
     }
 }
@@ -355,15 +388,25 @@ hipError_t launch_combine(int dtype, const RouteArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_combine_backward(int dtype, const RouteArgs& a, hipStream_t s) {
-    const uint32_t blocks = (uint32_t)(((int64_t)a.T * a.K + kWaves - 1) / kWaves);
+    // Four waves per pair while the pairs are too few to fill the device with one each
+    // (us, one wave -> four, H 7168 from an int8 checkpoint: 128 pairs 11.4 -> 5.1, 1024
+    // 12.6 -> 7.7, 2048 14.1 -> 12.6, 4096 17.5 -> 22.6, 8192 32.9 -> 42.8). A workgroup
+    // per token with all of its rows in flight read dout once but wrote in more places
+    // at a time: 8192 pairs of two choices 43 -> 58 to 66.
+    const int64_t pairs = (int64_t)a.T * a.K;
+    const bool few = pairs <= 2048;
+    const uint32_t blocks = (uint32_t)(few ? pairs : (pairs + kWaves - 1) / kWaves);
     const int per = a.out ? padding_blocks(a) : 0;
     const dim3 g(blocks + (uint32_t)(per * a.E)), b(kThreads);
+    auto go = [&](auto dt, auto src) {
+        constexpr int DT = decltype(dt)::value, SRC = decltype(src)::value;
+        if (few) hipLaunchKernelGGL((combine_backward_kernel<DT, SRC, kWaves>), g, b, 0, s, a, blocks, per);
+        else hipLaunchKernelGGL((combine_backward_kernel<DT, SRC, 1>), g, b, 0, s, a, blocks, per);
+    };
     auto from = [&](auto dt) {
-        constexpr int DT = decltype(dt)::value;
-        if (!a.packed) hipLaunchKernelGGL((combine_backward_kernel<DT, 0>), g, b, 0, s, a, blocks, per);
-        else if (a.format == FO_PACK_INT8)
-            hipLaunchKernelGGL((combine_backward_kernel<DT, 1 + FO_PACK_INT8>), g, b, 0, s, a, blocks, per);
-        else hipLaunchKernelGGL((combine_backward_kernel<DT, 1 + FO_PACK_E4M3>), g, b, 0, s, a, blocks, per);
+        if (!a.packed) go(dt, Int<0>());
+        else if (a.format == FO_PACK_INT8) go(dt, Int<1 + FO_PACK_INT8>());
+        else go(dt, Int<1 + FO_PACK_E4M3>());
     };
     if (dtype == FO_FP16) from(Int<FO_FP16>());
     else from(Int<FO_BF16>());
