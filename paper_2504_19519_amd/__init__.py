@@ -589,52 +589,52 @@ def _pick(table, key, what: str) -> int:
 _TYPES = {}          # element types that an argument takes, once a tensor has been seen
 
 
-def _types(kind):
-    """Torch dtypes of a kind of argument: the values' (FP16, BF16: that type or a 16-bit
+def _types():
+    """Torch dtypes of the kinds of arguments: values (FP16, BF16: that type or a 16-bit
     container), "f32", "i32", "ids", "u8"."""
-    if not _TYPES:
-        t = sys.modules["torch"]
-        bits = {t.int16, t.uint16}
-        _TYPES.update({FP16: {t.float16} | bits, BF16: {t.bfloat16} | bits, "f32": {t.float32},
-                       "i32": {t.int32, t.uint32}, "ids": {t.int32, t.int64}, "u8": {t.uint8, t.int8}})
-    return _TYPES[kind]
+    t = sys.modules["torch"]
+    bits = {t.int16, t.uint16}
+    _TYPES.update({FP16: {t.float16} | bits, BF16: {t.bfloat16} | bits, "f32": {t.float32},
+                   "i32": {t.int32, t.uint32}, "ids": {t.int32, t.int64}, "u8": {t.uint8, t.int8}})
+    return _TYPES
 
 
 class _Args:
     """Pointers of one row operator's arguments. Tensors are checked: on one GPU,
     the current one (and the stream's), of the dtype that the call takes, large
     enough, and contiguous or (matrices) with rows of unit stride. Raw pointers are
-    taken as given."""
+    taken as given. (Written out for few Python calls per tensor: they are what a call
+    on a few rows takes.)"""
 
-    __slots__ = ("dtype", "device")
+    __slots__ = ("dtype", "device", "stream")
 
     def __init__(self, dtype, stream):
         self.dtype = _pick(_DTYPES, dtype, "dtype")
-        self.device = None
-        torch = sys.modules.get("torch")
-        if torch is not None and torch.cuda.is_initialized():
-            self.device = torch.cuda.current_device()
-            at = getattr(stream, "device_index", self.device)
-            if at != self.device:
-                raise ValueError(f"stream: of device {at}, the current one is {self.device}")
+        self.device = None              # of the first tensor
+        self.stream = stream
 
-    def _other_device(self, d, what):
+    def _place(self, d, what):
+        """A tensor on a device other than the ones before it, or the first one."""
         if d < 0:
             raise ValueError(f"{what}: a tensor on the GPU is needed")
         if self.device is not None:
-            raise ValueError(f"{what}: on device {d}, the call runs on device {self.device}")
+            raise ValueError(f"{what}: on device {d}, other arguments are on device {self.device}")
+        current = sys.modules["torch"].cuda.current_device()
+        if d != current or (self.stream is not None and getattr(self.stream, "device_index", d) != d):
+            raise ValueError(f"{what}: on device {d}, not the current one ({current}) or the stream's")
         self.device = d
 
     def rows(self, x, M: int, N: int, ld, what: str):
         """(pointer, row distance) of a [M, N] matrix of 16-bit values."""
         if x is None:
             return None, N
-        if not hasattr(x, "get_device"):
+        try:
+            d = x.get_device()
+        except AttributeError:
             return _ptr(x), N if ld is None else int(ld)
-        d = x.get_device()
-        if d != self.device:
-            self._other_device(d, what)
-        if x.dtype not in _types(self.dtype):
+        if d != self.device or d < 0:
+            self._place(d, what)
+        if x.dtype not in (_TYPES or _types())[self.dtype]:
             raise ValueError(f"{what}: {x.dtype} values for {'bf16' if self.dtype else 'fp16'}")
         if ld is None and x.dim() == 2:
             have, length = x.shape
@@ -656,14 +656,15 @@ class _Args:
         """Pointer of `count` contiguous elements of a kind (None: the values')."""
         if x is None:
             return None
-        if not hasattr(x, "get_device"):
+        try:
+            d = x.get_device()
+        except AttributeError:
             return _ptr(x)
-        d = x.get_device()
-        if d != self.device:
-            self._other_device(d, what)
-        if x.dtype not in _types(self.dtype if kind is None else kind):
+        if d != self.device or d < 0:
+            self._place(d, what)
+        if x.dtype not in (_TYPES or _types())[self.dtype if kind is None else kind]:
             raise ValueError(f"{what}: elements of {x.dtype}")
-        if not x.is_contiguous() or x.numel() < count:
+        if x.numel() < count or not x.is_contiguous():
             raise ValueError(f"{what}: {count} contiguous elements are needed")
         return x.data_ptr()
 
@@ -671,11 +672,12 @@ class _Args:
         """(pointer, bytes) of a workspace; a raw pointer's size is not known and taken as enough."""
         if x is None:
             return None, 0
-        if not hasattr(x, "get_device"):
+        try:
+            d = x.get_device()
+        except AttributeError:
             return _ptr(x), (1 << 63) - 1
-        d = x.get_device()
-        if d != self.device:
-            self._other_device(d, what)
+        if d != self.device or d < 0:
+            self._place(d, what)
         if not x.is_contiguous():
             raise ValueError(f"{what}: contiguous memory is needed")
         return x.data_ptr(), x.numel() * x.element_size()

@@ -421,31 +421,34 @@ using Int = std::integral_constant<int, N>;
 
 // A form's constants, as go(chunks, threads, rows).
 template <int CH, int TH, int MAX, typename F>
-void for_rows(const NormForm& f, F go) {
+hipError_t for_rows(const NormForm& f, F go) {
     if constexpr (MAX > 1) {
         if (f.rows < MAX) return for_rows<CH, TH, MAX / 2>(f, go);
     }
-    go(Int<CH>(), Int<TH>(), Int<MAX>());
+    return go(Int<CH>(), Int<TH>(), Int<MAX>());
 }
 template <typename F>
-void for_forward(const NormForm& f, F go) {
-    if (f.threads == 64) for_rows<2, 64, 8>(f, go);
-    else if (f.threads == 128) for_rows<2, 128, 4>(f, go);
-    else if (f.threads == 256) for_rows<2, 256, 2>(f, go);
-    else if (f.threads == 512) for_rows<2, 512, 1>(f, go);
-    else if (f.chunks == 2) for_rows<2, 1024, 1>(f, go);
-    else for_rows<4, 1024, 1>(f, go);
+hipError_t for_forward(const NormForm& f, F go) {
+    switch (f.threads) {
+        case 64: return for_rows<2, 64, 8>(f, go);
+        case 128: return for_rows<2, 128, 4>(f, go);
+        case 256: return for_rows<2, 256, 2>(f, go);
+        case 512: return for_rows<2, 512, 1>(f, go);
+        default: return f.chunks == 2 ? for_rows<2, 1024, 1>(f, go) : for_rows<4, 1024, 1>(f, go);
+    }
 }
 template <typename F>
-void for_backward(const NormForm& f, F go) {
-    if (f.threads == 64) for_rows<1, 64, 16>(f, go);
-    else if (f.threads == 128) for_rows<1, 128, 8>(f, go);
-    else if (f.threads == 256) for_rows<1, 256, 4>(f, go);
-    else if (f.threads == 512) for_rows<1, 512, 2>(f, go);
-    else if (f.threads == 768) for_rows<2, 768, 1>(f, go);
-    else if (f.chunks == 1) for_rows<1, 1024, 1>(f, go);
-    else if (f.chunks == 2) for_rows<2, 1024, 1>(f, go);
-    else for_rows<4, 1024, 1>(f, go);
+hipError_t for_backward(const NormForm& f, F go) {
+    switch (f.threads) {
+        case 64: return for_rows<1, 64, 16>(f, go);
+        case 128: return for_rows<1, 128, 8>(f, go);
+        case 256: return for_rows<1, 256, 4>(f, go);
+        case 512: return for_rows<1, 512, 2>(f, go);
+        case 768: return for_rows<2, 768, 1>(f, go);
+        default:
+            return f.chunks == 1 ? for_rows<1, 1024, 1>(f, go)
+                   : f.chunks == 2 ? for_rows<2, 1024, 1>(f, go) : for_rows<4, 1024, 1>(f, go);
+    }
 }
 
 // As many rows at a time, in a workgroup of up to `threads`, as leave every one of
@@ -486,46 +489,39 @@ NormForm norm_backward_form(int64_t M, int64_t N) {
 
 hipError_t launch_norm_forward(int dtype, const NormArgs& a, hipStream_t s) {
     const NormForm f = norm_forward_form(a.M, a.N);
-    for_forward(f, [&](auto ch, auto th, auto rows) {
+    return for_forward(f, [&](auto ch, auto th, auto rows) {
         constexpr int CH = decltype(ch)::value, TH = decltype(th)::value, ROWS = decltype(rows)::value;
-        const dim3 g(f.blocks), b(TH * ROWS);
-        if (dtype == FO_FP16) hipLaunchKernelGGL((norm_forward_kernel<FO_FP16, CH, TH, ROWS>), g, b, 0, s, a);
-        else hipLaunchKernelGGL((norm_forward_kernel<FO_BF16, CH, TH, ROWS>), g, b, 0, s, a);
+        return launch(dtype == FO_FP16 ? norm_forward_kernel<FO_FP16, CH, TH, ROWS>
+                                       : norm_forward_kernel<FO_BF16, CH, TH, ROWS>,
+                      f.blocks, TH * ROWS, s, a);
     });
-    return hipGetLastError();
 }
 
 hipError_t launch_norm_backward(int dtype, const NormArgs& a, float* dgamma, float* dbeta, hipStream_t s) {
     const NormForm f = norm_backward_form(a.M, a.N);
-    if (a.M > 0) {
-        for_backward(f, [&](auto ch, auto th, auto rows) {
+    hipError_t e = hipSuccess;
+    if (a.M > 0)
+        e = for_backward(f, [&](auto ch, auto th, auto rows) {
             constexpr int CH = decltype(ch)::value, TH = decltype(th)::value, ROWS = decltype(rows)::value;
             // rows ahead, as the registers of the workgroup's waves allow
             constexpr int AHEAD = CH == 1 ? 3 : TH == 768 ? 2 : 1;
-            const dim3 g(f.blocks), b(TH * ROWS);
-            auto go = [&](auto dt, auto src) {
-                hipLaunchKernelGGL((norm_backward_kernel<decltype(dt)::value, decltype(src)::value, CH, TH, ROWS, AHEAD>), g, b,
-                                   0, s, a);
-            };
-            const int src = a.packed ? 1 + a.format : 0;
             auto from = [&](auto dt) {
-                if (src == 0) go(dt, Int<0>());
-                else if (src == 1) go(dt, Int<1>());
-                else go(dt, Int<2>());
+                constexpr int DT = decltype(dt)::value;
+                return launch(!a.packed ? norm_backward_kernel<DT, 0, CH, TH, ROWS, AHEAD>
+                              : a.format == FO_PACK_INT8
+                                  ? norm_backward_kernel<DT, 1 + FO_PACK_INT8, CH, TH, ROWS, AHEAD>
+                                  : norm_backward_kernel<DT, 1 + FO_PACK_E4M3, CH, TH, ROWS, AHEAD>,
+                              f.blocks, TH * ROWS, s, a);
             };
-            if (dtype == FO_FP16) from(Int<FO_FP16>());
-            else from(Int<FO_BF16>());
+            return dtype == FO_FP16 ? from(Int<FO_FP16>()) : from(Int<FO_BF16>());
         });
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    if (dgamma || dbeta) {
+    if (e == hipSuccess && (dgamma || dbeta)) {
         const int count = a.M > 0 ? (int)f.blocks : 0;
         const int64_t per = (norm_partial_cols(a.N) + kReduceCols - 1) / kReduceCols;
-        hipLaunchKernelGGL(norm_reduce_kernel, dim3((uint32_t)(per * (dgamma && dbeta ? 2 : 1))), dim3(kReduceThreads), 0,
-                           s, a.partial, count, a.N, dgamma, dbeta);
+        e = launch(norm_reduce_kernel, (uint32_t)(per * (dgamma && dbeta ? 2 : 1)), kReduceThreads, s, a.partial, count, a.N,
+                   dgamma, dbeta);
     }
-    return hipGetLastError();
+    return e;
 }
 
 }  // namespace fo

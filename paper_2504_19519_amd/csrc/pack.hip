@@ -94,34 +94,22 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(const PackArgs a, uint
 
 uint32_t slices_of(int64_t N) { return (uint32_t)(N / 8 > kSlice ? (N / 8 + kSlice - 1) / kSlice : 1); }
 
-template <typename F>
-hipError_t for_types(int dtype, int format, F f) {
-    if (dtype == FO_FP16) {
-        if (format == FO_PACK_INT8) f(std::integral_constant<int, FO_FP16>(), std::integral_constant<int, FO_PACK_INT8>());
-        else f(std::integral_constant<int, FO_FP16>(), std::integral_constant<int, FO_PACK_E4M3>());
-    } else {
-        if (format == FO_PACK_INT8) f(std::integral_constant<int, FO_BF16>(), std::integral_constant<int, FO_PACK_INT8>());
-        else f(std::integral_constant<int, FO_BF16>(), std::integral_constant<int, FO_PACK_E4M3>());
-    }
-    return hipGetLastError();
-}
+uint32_t workgroups(const PackArgs& a) { return (uint32_t)((a.M * slices_of(a.N) + kThreads / 64 - 1) / (kThreads / 64)); }
 
 }  // namespace
 
 hipError_t launch_pack(int dtype, int format, const PackArgs& a, hipStream_t s) {
-    const uint32_t slices = slices_of(a.N);
-    const dim3 g((uint32_t)((a.M * slices + 3) / 4)), b(kThreads);
-    return for_types(dtype, format, [&](auto dt, auto fmt) {
-        hipLaunchKernelGGL((pack_kernel<decltype(dt)::value, decltype(fmt)::value>), g, b, 0, s, a, slices);
-    });
+    const bool int8 = format == FO_PACK_INT8;
+    return launch(dtype == FO_FP16 ? (int8 ? pack_kernel<FO_FP16, FO_PACK_INT8> : pack_kernel<FO_FP16, FO_PACK_E4M3>)
+                                   : (int8 ? pack_kernel<FO_BF16, FO_PACK_INT8> : pack_kernel<FO_BF16, FO_PACK_E4M3>),
+                  workgroups(a), kThreads, s, a, slices_of(a.N));
 }
 
 hipError_t launch_unpack(int dtype, int format, const PackArgs& a, hipStream_t s) {
-    const uint32_t slices = slices_of(a.N);
-    const dim3 g((uint32_t)((a.M * slices + 3) / 4)), b(kThreads);
-    return for_types(dtype, format, [&](auto dt, auto fmt) {
-        hipLaunchKernelGGL((unpack_kernel<decltype(dt)::value, decltype(fmt)::value>), g, b, 0, s, a, slices);
-    });
+    const bool int8 = format == FO_PACK_INT8;
+    return launch(dtype == FO_FP16 ? (int8 ? unpack_kernel<FO_FP16, FO_PACK_INT8> : unpack_kernel<FO_FP16, FO_PACK_E4M3>)
+                                   : (int8 ? unpack_kernel<FO_BF16, FO_PACK_INT8> : unpack_kernel<FO_BF16, FO_PACK_E4M3>),
+                  workgroups(a), kThreads, s, a, slices_of(a.N));
 }
 
 }  // namespace fo

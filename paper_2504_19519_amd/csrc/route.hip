@@ -20,7 +20,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "rowops.h"
 #include "rows.h"
@@ -341,9 +340,6 @@ uint32_t slices_of(int64_t H) { return (uint32_t)std::max<int64_t>(1, (H / 8 + 6
 // Workgroups per expert that zero padding rows.
 int padding_blocks(const RouteArgs& a) { return a.offsets ? std::max(1, std::min(16, 256 / a.E)) : 0; }
 
-template <int N>
-using Int = std::integral_constant<int, N>;
-
 }  // namespace
 
 int64_t sort_blocks(int64_t pairs) {
@@ -354,37 +350,41 @@ hipError_t launch_sort(const SortArgs& a, hipStream_t s) {
     const int64_t blocks = sort_blocks(a.pairs);
     // whole steps of every wave
     const int64_t run = ((a.pairs + blocks - 1) / blocks + kSortThreads - 1) / kSortThreads * kSortThreads;
-    const dim3 g((uint32_t)blocks), b(kSortThreads);
-    auto go = [&](auto id) {
-        using ID = decltype(id);
-        if (blocks > 1) hipLaunchKernelGGL(sort_count_kernel<ID>, g, b, 0, s, a, run);
-        hipLaunchKernelGGL(sort_place_kernel<ID>, g, b, 0, s, a, run);
-    };
-    if (a.id_bytes == 8) go(int64_t{});
-    else go(int32_t{});
-    return hipGetLastError();
+    const bool wide = a.id_bytes == 8;
+    if (blocks > 1) {
+        const hipError_t e = launch(wide ? sort_count_kernel<int64_t> : sort_count_kernel<int32_t>, (uint32_t)blocks,
+                                    kSortThreads, s, a, run);
+        if (e != hipSuccess) return e;
+    }
+    return launch(wide ? sort_place_kernel<int64_t> : sort_place_kernel<int32_t>, (uint32_t)blocks, kSortThreads, s, a, run);
 }
 
 hipError_t launch_permute(const RouteArgs& a, hipStream_t s) {
     const uint32_t slices = slices_of(a.H);
     const uint32_t blocks = (uint32_t)(((int64_t)a.T * slices + kWaves - 1) / kWaves);
     const int per = padding_blocks(a);
-    hipLaunchKernelGGL(permute_kernel, dim3(blocks + (uint32_t)per * a.E), dim3(kThreads), 0, s, a, slices, blocks, per);
-    return hipGetLastError();
+    return launch(permute_kernel, blocks + (uint32_t)(per * a.E), kThreads, s, a, slices, blocks, per);
 }
 
 hipError_t launch_combine(int dtype, const RouteArgs& a, hipStream_t s) {
     const uint32_t slices = slices_of(a.H);
-    const dim3 g((uint32_t)(((int64_t)a.T * slices + kWaves - 1) / kWaves)), b(kThreads);
-    auto from = [&](auto dt) {
-        constexpr int DT = decltype(dt)::value;
-        if (!a.packed) hipLaunchKernelGGL((combine_kernel<DT, -1>), g, b, 0, s, a, slices);
-        else if (a.format == FO_PACK_INT8) hipLaunchKernelGGL((combine_kernel<DT, FO_PACK_INT8>), g, b, 0, s, a, slices);
-        else hipLaunchKernelGGL((combine_kernel<DT, FO_PACK_E4M3>), g, b, 0, s, a, slices);
-    };
-    if (dtype == FO_FP16) from(Int<FO_FP16>());
-    else from(Int<FO_BF16>());
-    return hipGetLastError();
+    const int kept = a.packed ? a.format : -1;
+    return launch(dtype == FO_FP16 ? (kept < 0                ? combine_kernel<FO_FP16, -1>
+                                      : kept == FO_PACK_INT8 ? combine_kernel<FO_FP16, FO_PACK_INT8>
+                                                             : combine_kernel<FO_FP16, FO_PACK_E4M3>)
+                                   : (kept < 0                ? combine_kernel<FO_BF16, -1>
+                                      : kept == FO_PACK_INT8 ? combine_kernel<FO_BF16, FO_PACK_INT8>
+                                                             : combine_kernel<FO_BF16, FO_PACK_E4M3>),
+                  (uint32_t)(((int64_t)a.T * slices + kWaves - 1) / kWaves), kThreads, s, a, slices);
+}
+
+template <int DT, int WAVES>
+static hipError_t launch_back(const RouteArgs& a, uint32_t blocks, hipStream_t s) {
+    const int per = a.out ? padding_blocks(a) : 0;
+    return launch(!a.packed                     ? combine_backward_kernel<DT, 0, WAVES>
+                  : a.format == FO_PACK_INT8 ? combine_backward_kernel<DT, 1 + FO_PACK_INT8, WAVES>
+                                             : combine_backward_kernel<DT, 1 + FO_PACK_E4M3, WAVES>,
+                  blocks + (uint32_t)(per * a.E), kThreads, s, a, blocks, per);
 }
 
 hipError_t launch_combine_backward(int dtype, const RouteArgs& a, hipStream_t s) {
@@ -394,23 +394,11 @@ hipError_t launch_combine_backward(int dtype, const RouteArgs& a, hipStream_t s)
     // per token with all of its rows in flight read dout once but wrote in more places
     // at a time: 8192 pairs of two choices 43 -> 58 to 66.
     const int64_t pairs = (int64_t)a.T * a.K;
-    const bool few = pairs <= 2048;
-    const uint32_t blocks = (uint32_t)(few ? pairs : (pairs + kWaves - 1) / kWaves);
-    const int per = a.out ? padding_blocks(a) : 0;
-    const dim3 g(blocks + (uint32_t)(per * a.E)), b(kThreads);
-    auto go = [&](auto dt, auto src) {
-        constexpr int DT = decltype(dt)::value, SRC = decltype(src)::value;
-        if (few) hipLaunchKernelGGL((combine_backward_kernel<DT, SRC, kWaves>), g, b, 0, s, a, blocks, per);
-        else hipLaunchKernelGGL((combine_backward_kernel<DT, SRC, 1>), g, b, 0, s, a, blocks, per);
-    };
-    auto from = [&](auto dt) {
-        if (!a.packed) go(dt, Int<0>());
-        else if (a.format == FO_PACK_INT8) go(dt, Int<1 + FO_PACK_INT8>());
-        else go(dt, Int<1 + FO_PACK_E4M3>());
-    };
-    if (dtype == FO_FP16) from(Int<FO_FP16>());
-    else from(Int<FO_BF16>());
-    return hipGetLastError();
+    if (pairs <= 2048)
+        return dtype == FO_FP16 ? launch_back<FO_FP16, kWaves>(a, (uint32_t)pairs, s)
+                                : launch_back<FO_BF16, kWaves>(a, (uint32_t)pairs, s);
+    const uint32_t blocks = (uint32_t)((pairs + kWaves - 1) / kWaves);
+    return dtype == FO_FP16 ? launch_back<FO_FP16, 1>(a, blocks, s) : launch_back<FO_BF16, 1>(a, blocks, s);
 }
 
 }  // namespace fo

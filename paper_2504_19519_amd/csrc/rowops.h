@@ -9,6 +9,17 @@
 
 namespace fo {
 
+// Launches a kernel by one call of the runtime, which also says whether it went well
+// (the launch syntax is three calls, and its error a fourth that would report earlier
+// ones too).
+template <typename... Params, typename... Args>
+hipError_t launch(void (*kernel)(Params...), dim3 grid, dim3 threads, hipStream_t s, const Args&... args) {
+    return [&](Params... params) {
+        void* at[] = {static_cast<void*>(&params)...};
+        return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, threads, at, 0, s);
+    }(args...);
+}
+
 // A checkpoint of a matrix with N columns: blocks of 32 along a row.
 inline int64_t pack_blocks(int64_t N) { return (N + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK; }
 
