@@ -29,17 +29,25 @@
 namespace fo {
 namespace {
 
+// Which of the workgroup's rows a thread works on. A wave that lies within one row
+// has its number in a scalar register, and the row's addresses too.
+template <int TH>
+__device__ __forceinline__ int row_group() {
+    const int group = threadIdx.x / TH;
+    return TH < 64 ? group : __builtin_amdgcn_readfirstlane(group);
+}
+
 // ROWS rows at a time, TH threads each. Every thread keeps its columns of gamma and
 // beta, and the next row's loads are issued ahead of this row's sums. Where a row
 // has several waves each takes the mean of its own values and the sum of their
 // squared differences from it, and one meeting joins them:
 //   sum of (x - mu)^2 = sum over waves of (their sum + n_w (mu_w - mu)^2).
+// Rows of up to half a wave share waves (a checkpoint's last block then has to be whole).
 template <int DT, int CH, int TH, int ROWS>
 __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs a) {
-    constexpr int kRowWaves = TH / 64;
+    constexpr int kRowWaves = TH / 64;              // 0: several rows in a wave
     __shared__ float s_sum[2][2][TH * ROWS / 64];
-    // (a wave lies within one row: its row is the same for every lane)
-    const int lane = threadIdx.x % TH, group = __builtin_amdgcn_readfirstlane(threadIdx.x / TH);
+    const int lane = threadIdx.x % TH, group = row_group<TH>();
     const int full = (int)(a.N >> 3), tail = (int)(a.N & 7);
     const bool has_tail = lane < tail;
     const int64_t blocks = (a.N + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK, step = (int64_t)gridDim.x * ROWS;
@@ -71,7 +79,7 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
     }
     if (a.gamma && has_tail) gamma_t = to_f32<DT>(a.gamma[8 * full + lane]);
     if (a.beta && has_tail) beta_t = to_f32<DT>(a.beta[8 * full + lane]);
-    count = wave_sum(count * scale);                // of this wave, scaled like the sums
+    count = wave_sum(count * scale);                // of this wave, scaled like the sums (kRowWaves > 1)
     const float inv_count = count > 0.0f ? 1.0f / count : 0.0f;
     float wave_count = 0.0f;                        // lane w: of the row's wave w
     if constexpr (kRowWaves > 1) {
@@ -117,7 +125,7 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
                 }
             }
             // (read again here, ahead of any store to y, which may be x)
-            if (a.N % FO_PACK_BLOCK && lane < 64) {
+            if (TH >= 64 && a.N % FO_PACK_BLOCK && lane < 64) {
                 const uint16_t* row = a.x + i * a.ldx;
                 if (a.format == FO_PACK_INT8) pack_last<DT, FO_PACK_INT8>(row, a.N, lane, packed, scales);
                 else pack_last<DT, FO_PACK_E4M3>(row, a.N, lane, packed, scales);
@@ -131,7 +139,7 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
             for (int t = 0; t < CH; ++t)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum += x[t][e];
-            sum = wave_sum(sum * scale);
+            sum = lanes_sum<(TH < 64 ? TH : 64)>(sum * scale);
             mean = kRowWaves > 1 ? sum * inv_count : mean_of(sum);
         }
 #pragma unroll
@@ -142,7 +150,7 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
             if (lane + TH * t < full) square += q;
         }
         if (has_tail) square += (xt - mean) * (xt - mean);
-        square = wave_sum(square * scale);
+        square = lanes_sum<(TH < 64 ? TH : 64)>(square * scale);
         if constexpr (kRowWaves > 1) {
             // (two sets of words, so that one barrier per row is enough)
             const int set = (int)(round & 1), wave = threadIdx.x >> 6, w = threadIdx.x & 63;
@@ -198,11 +206,10 @@ struct RowPart {
 // there are few workgroups' sums to add.
 template <int DT, int SRC, int CH, int TH, int ROWS, int AHEAD>
 __global__ __launch_bounds__(TH * ROWS) void norm_backward_kernel(const NormArgs a) {
-    constexpr int kWaves = TH * ROWS / 64, kRowWaves = TH / 64;
+    constexpr int kWaves = TH * ROWS / 64, kRowWaves = TH / 64;     // (0: several rows in a wave)
     __shared__ float s_sum[2][2][kWaves];
     __shared__ float s_cols[ROWS > 1 ? ROWS / 2 : 1][ROWS > 1 ? 8 * CH + 1 : 1][ROWS > 1 ? TH : 1];
-    // (a wave lies within one row: its row is the same for every lane)
-    const int lane = threadIdx.x % TH, group = __builtin_amdgcn_readfirstlane(threadIdx.x / TH);
+    const int lane = threadIdx.x % TH, group = row_group<TH>();
     const int full = (int)(a.N >> 3), tail = (int)(a.N & 7);
     const float inv_n = 1.0f / (float)a.N;
     const bool has_tail = lane < tail;
@@ -303,7 +310,12 @@ __global__ __launch_bounds__(TH * ROWS) void norm_backward_kernel(const NormArgs
             s2 += gt * tt;
         }
         load(i + AHEAD * step, next);
-        wave_sums(s1, s2);
+        if constexpr (TH < 64) {
+            s1 = lanes_sum<TH>(s1);
+            s2 = lanes_sum<TH>(s2);
+        } else {
+            wave_sums(s1, s2);
+        }
         if constexpr (kRowWaves > 1) {
             // (two sets of words, so that one barrier per row is enough)
             const int set = (int)(n & 1), wave = threadIdx.x >> 6;
@@ -384,9 +396,9 @@ __global__ __launch_bounds__(TH * ROWS) void norm_backward_kernel(const NormArgs
     if (a.with_beta) add_up(dbeta, dbeta_t, partial + norm_partial_cols(a.N));
 }
 
-// dgamma and dbeta: the sums of `count` workgroups' sums (2 * cols each), 64 columns
-// per workgroup: 16 threads of four columns, 64 rows at a time.
-constexpr int kReduceThreads = 1024, kReduceCols = 64;
+// dgamma and dbeta: the sums of `count` workgroups' sums (2 * cols each), 32 columns
+// per workgroup: 8 threads of four columns, 32 rows at a time.
+constexpr int kReduceThreads = 256, kReduceCols = 32;
 __global__ __launch_bounds__(kReduceThreads) void norm_reduce_kernel(const float* partial, int count, int64_t N,
                                                                       float* dgamma, float* dbeta) {
     constexpr int kRows = kReduceThreads / (kReduceCols / 4);
@@ -398,7 +410,7 @@ __global__ __launch_bounds__(kReduceThreads) void norm_reduce_kernel(const float
     const float* from = partial + (beta ? cols : 0) + c;
     f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
     if (c < cols) {
-#pragma unroll 4
+#pragma unroll 8
         for (int g = part; g < count; g += kRows) sum += *reinterpret_cast<const f32x4_t*>(from + (int64_t)g * 2 * cols);
     }
 #pragma unroll
@@ -419,56 +431,66 @@ __global__ __launch_bounds__(kReduceThreads) void norm_reduce_kernel(const float
 template <int N>
 using Int = std::integral_constant<int, N>;
 
-// A form's constants, as go(chunks, threads, rows).
-template <int CH, int TH, int MAX, typename F>
+// A form's constants, as go(chunks, threads, rows): rows of MAX, MAX / STEP, .. MIN.
+template <int CH, int TH, int MAX, int MIN, int STEP, typename F>
 hipError_t for_rows(const NormForm& f, F go) {
-    if constexpr (MAX > 1) {
-        if (f.rows < MAX) return for_rows<CH, TH, MAX / 2>(f, go);
+    if constexpr (MAX > MIN) {
+        if (f.rows < MAX) return for_rows<CH, TH, MAX / STEP, MIN, STEP>(f, go);
     }
     return go(Int<CH>(), Int<TH>(), Int<MAX>());
 }
 template <typename F>
 hipError_t for_forward(const NormForm& f, F go) {
     switch (f.threads) {
-        case 64: return for_rows<2, 64, 8>(f, go);
-        case 128: return for_rows<2, 128, 4>(f, go);
-        case 256: return for_rows<2, 256, 2>(f, go);
-        case 512: return for_rows<2, 512, 1>(f, go);
-        default: return f.chunks == 2 ? for_rows<2, 1024, 1>(f, go) : for_rows<4, 1024, 1>(f, go);
+        case 8: return for_rows<2, 8, 64, 16, 4>(f, go);
+        case 16: return for_rows<2, 16, 32, 8, 4>(f, go);
+        case 32: return for_rows<2, 32, 16, 4, 4>(f, go);
+        case 64: return for_rows<2, 64, 8, 1, 2>(f, go);
+        case 128: return for_rows<2, 128, 4, 1, 2>(f, go);
+        case 256: return for_rows<2, 256, 2, 1, 2>(f, go);
+        case 512: return for_rows<2, 512, 1, 1, 2>(f, go);
+        default: return f.chunks == 2 ? for_rows<2, 1024, 1, 1, 2>(f, go) : for_rows<4, 1024, 1, 1, 2>(f, go);
     }
 }
 template <typename F>
 hipError_t for_backward(const NormForm& f, F go) {
     switch (f.threads) {
-        case 64: return for_rows<1, 64, 16>(f, go);
-        case 128: return for_rows<1, 128, 8>(f, go);
-        case 256: return for_rows<1, 256, 4>(f, go);
-        case 512: return for_rows<1, 512, 2>(f, go);
-        case 768: return for_rows<2, 768, 1>(f, go);
+        case 8: return for_rows<1, 8, 128, 32, 4>(f, go);
+        case 16: return for_rows<1, 16, 64, 16, 4>(f, go);
+        case 32: return for_rows<1, 32, 32, 8, 4>(f, go);
+        case 64: return for_rows<1, 64, 16, 1, 2>(f, go);
+        case 128: return for_rows<1, 128, 8, 1, 2>(f, go);
+        case 256: return for_rows<1, 256, 4, 1, 2>(f, go);
+        case 512: return for_rows<1, 512, 2, 1, 2>(f, go);
+        case 768: return for_rows<2, 768, 1, 1, 2>(f, go);
         default:
-            return f.chunks == 1 ? for_rows<1, 1024, 1>(f, go)
-                   : f.chunks == 2 ? for_rows<2, 1024, 1>(f, go) : for_rows<4, 1024, 1>(f, go);
+            return f.chunks == 1 ? for_rows<1, 1024, 1, 1, 2>(f, go)
+                   : f.chunks == 2 ? for_rows<2, 1024, 1, 1, 2>(f, go) : for_rows<4, 1024, 1, 1, 2>(f, go);
     }
 }
 
 // As many rows at a time, in a workgroup of up to `threads`, as leave every one of
-// `units` workgroups some.
+// `units` workgroups some; where rows share waves, all that fit or a quarter.
 void set_rows(NormForm& f, int64_t M, int threads, int64_t units) {
-    f.rows = 1;
-    while (f.rows * 2 * f.threads <= threads && f.rows * 2 * units <= M) f.rows *= 2;
+    const int most = std::max(1, threads / f.threads);
+    const int least = f.threads < 64 ? most / 4 : 1, step = f.threads < 64 ? 4 : 2;
+    f.rows = most;
+    while (f.rows > least && f.rows * units > M) f.rows /= step;
     f.blocks = (uint32_t)std::min<int64_t>((M + f.rows - 1) / f.rows, units);
 }
 
 }  // namespace
 
-// Forward: three workgroups of eight waves per compute unit (8192x8192 fp16 54 us,
-// 16384x4096 bf16 with a checkpoint 58; one of 16 waves, on more rows, 66 for the
+// Forward: three workgroups of eight waves per compute unit (8192x8192 fp16 52 us,
+// 16384x4096 bf16 with a checkpoint 56; one of 16 waves, on more rows, 66 for the
 // second; registers held down to two of 16 waves 69 and 83; a workgroup per row and
 // nothing ahead 60 and 61). Past 8192 columns, where a row has 16 waves and they fit
-// once: one (1280x12288 20.1; 22.8 with three, two of them waiting).
-NormForm norm_forward_form(int64_t M, int64_t N) {
+// once: one (1280x12288 18.9; 22.8 with three, two of them waiting).
+NormForm norm_forward_form(int64_t M, int64_t N, bool pack) {
+    const bool share = !pack || N % FO_PACK_BLOCK == 0;
     NormForm f{};
-    f.threads = N <= 1024 ? 64 : N <= 2048 ? 128 : N <= 4096 ? 256 : N <= 8192 ? 512 : 1024;
+    f.threads = share && N <= 512 ? (N <= 128 ? 8 : N <= 256 ? 16 : 32)
+              : N <= 1024 ? 64 : N <= 2048 ? 128 : N <= 4096 ? 256 : N <= 8192 ? 512 : 1024;
     f.chunks = N <= 16384 ? 2 : 4;
     set_rows(f, M, 512, N <= 8192 ? 768 : 256);
     return f;
@@ -480,15 +502,15 @@ NormForm norm_forward_form(int64_t M, int64_t N) {
 // chunks and one row ahead 66, two rows ahead do not fit and take 140).
 NormForm norm_backward_form(int64_t M, int64_t N) {
     NormForm f{};
-    f.threads = N <= 512 ? 64 : N <= 1024 ? 128 : N <= 2048 ? 256 : N <= 4096 ? 512 : N <= 8192 ? 1024
-              : N <= 12288 ? 768 : 1024;
+    f.threads = N <= 64 ? 8 : N <= 128 ? 16 : N <= 256 ? 32 : N <= 512 ? 64 : N <= 1024 ? 128 : N <= 2048 ? 256
+              : N <= 4096 ? 512 : N <= 8192 ? 1024 : N <= 12288 ? 768 : 1024;
     f.chunks = N <= 8192 ? 1 : N <= 16384 ? 2 : 4;
     set_rows(f, M, 1024, 256);
     return f;
 }
 
 hipError_t launch_norm_forward(int dtype, const NormArgs& a, hipStream_t s) {
-    const NormForm f = norm_forward_form(a.M, a.N);
+    const NormForm f = norm_forward_form(a.M, a.N, a.packed != nullptr);
     return for_forward(f, [&](auto ch, auto th, auto rows) {
         constexpr int CH = decltype(ch)::value, TH = decltype(th)::value, ROWS = decltype(rows)::value;
         return launch(dtype == FO_FP16 ? norm_forward_kernel<FO_FP16, CH, TH, ROWS>

@@ -65,6 +65,27 @@ __device__ __forceinline__ float wave_sum(float v) {
     return bit_cast<float>(__builtin_amdgcn_readlane(bit_cast<int>(v), 63));
 }
 
+// Sum over TH neighbouring lanes (8, 16, 32 or all 64), the same in each of them. Lanes
+// change places within four (quad_perm [1, 0, 3, 2], [2, 3, 0, 1]), eight and sixteen
+// (row_half_mirror, row_mirror), and rows of sixteen by the swap of neighbouring ones.
+template <int TH>
+__device__ __forceinline__ float lanes_sum(float v) {
+    if constexpr (TH == 64) {
+        return wave_sum(v);
+    } else {
+        v = add_moved<0xB1, 0xF>(v);
+        v = add_moved<0x4E, 0xF>(v);
+        v = add_moved<0x141, 0xF>(v);
+        if constexpr (TH > 8) v = add_moved<0x140, 0xF>(v);
+        if constexpr (TH > 16) {
+            const u32x2_t swapped = bit_cast<u32x2_t>(
+                __builtin_amdgcn_permlane16_swap(bit_cast<uint32_t>(v), bit_cast<uint32_t>(v), false, false));
+            v = bit_cast<float>(swapped[0]) + bit_cast<float>(swapped[1]);
+        }
+        return v;
+    }
+}
+
 // Two sums over the 64 lanes for little more than one: the halves change places, so
 // that the lower lanes go on with a's sum and the upper ones with b's.
 __device__ __forceinline__ void wave_sums(float& a, float& b) {
