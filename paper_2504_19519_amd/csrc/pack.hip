@@ -1,10 +1,13 @@
 // 8-bit checkpoints: pack and unpack, bound by memory.
 //
-// A wave takes kAhead times 64 chunks of eight values of one row, all of their loads
-// in flight together; four lanes share a block's scale. The 16-bit side goes past the
-// caches in both directions, so that the codes stay: 8192x14336 bf16 to int8 and back
-// 59 + 51 us (6.0 and 6.9 TB/s; with cached loads 62 + 55, cached stores too 77 + 60,
-// one chunk per lane and cached 71 + 59).
+// Four lanes share a block of 32 values and its scale, a chunk of eight each; a
+// thread takes kAhead chunks, a workgroup's width apart, with their loads in flight
+// together. The chunks of all rows are numbered through, so that short rows fill
+// waves as long ones do; rows without gaps between them are one row.
+//
+// The 16-bit side goes past the caches in both directions, so that the codes stay:
+// 8192x14336 bf16 to int8 and back 59 + 51 us (6.0 and 6.9 TB/s; with cached loads
+// 62 + 55, cached stores too 77 + 60, one chunk per lane and cached 71 + 59).
 #include <hip/hip_runtime.h>
 
 #include "rowops.h"
@@ -15,101 +18,110 @@ namespace {
 
 constexpr int kThreads = 256;
 
-constexpr int kAhead = 2, kSlice = 64 * kAhead;      // chunks of one wave
+constexpr int kAhead = 2;
 
-// This wave's row and first chunk. 32 bits: the host sees to the number of waves.
-struct Slice {
+// Chunk `at` of the matrix: its row and its place in it.
+struct Chunk {
     int64_t i;
-    int c0;
-    bool last;
+    uint32_t c;
 };
-__device__ __forceinline__ Slice slice_of(uint32_t slices) {
-    const uint32_t unit = blockIdx.x * (kThreads / 64) + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t i = unit / slices, s = unit - i * slices;
-    return {(int64_t)i, (int)(s * kSlice), s == slices - 1};
+__device__ __forceinline__ Chunk chunk_of(const PackArgs& a, uint32_t at, uint32_t per_row) {
+    if (a.M == 1) return {0, at};
+    const uint32_t i = at / per_row;
+    return {(int64_t)i, at - i * per_row};
 }
 
+// `chunks` in all, `per_row` (a multiple of four) in a row's blocks.
 template <int DT, int FMT>
-__global__ __launch_bounds__(kThreads) void pack_kernel(const PackArgs a, uint32_t slices) {
-    const int lane = threadIdx.x & 63;
-    const Slice s = slice_of(slices);
-    if (s.i >= a.M) return;
-    const int64_t blocks = (a.N + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK;
-    const int whole = (int)(a.N / FO_PACK_BLOCK) * 4;           // chunks of whole blocks
-    const uint16_t* row = a.x + s.i * a.ldx;
-    uint8_t* packed = a.packed + s.i * blocks * FO_PACK_BLOCK;
-    uint8_t* scales = a.scales + s.i * blocks;
+__global__ __launch_bounds__(kThreads) void pack_kernel(const PackArgs a, uint32_t chunks, uint32_t per_row) {
+    const uint32_t first = blockIdx.x * (kThreads * kAhead) + threadIdx.x;
     u32x4_t v[kAhead];
+    Chunk at[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-        const int c = s.c0 + 64 * j + lane;
-        if (c < whole) v[j] = stream_load8(row + 8 * (int64_t)c);
-    }
+        const uint32_t q = first + j * kThreads;
+        v[j] = u32x4_t{0u, 0u, 0u, 0u};
+        if (q >= chunks) continue;
+        at[j] = chunk_of(a, q, per_row);
+        const int64_t n = 8 * (int64_t)at[j].c;
+        const uint16_t* from = a.x + at[j].i * a.ldx + n;
+        if (n + 8 <= a.N) {
+            v[j] = stream_load8(from);
+        } else {
+            // the row's end: what is left of it, then zeros
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-        const int c = s.c0 + 64 * j + lane;
-        if (c < whole) {
-            float f[8];
-            widen<DT>(v[j], f);
-            pack_chunk<DT, FMT>(f, c, packed, scales);
+            for (int e = 0; e < 7; ++e)
+                if (n + e < a.N) v[j][e >> 1] |= (uint32_t)from[e] << (16 * (e & 1));
         }
     }
-    if (s.last && a.N % FO_PACK_BLOCK) pack_last<DT, FMT>(row, a.N, lane, packed, scales);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+        if (first + j * kThreads >= chunks) continue;       // (four lanes of a block at once)
+        float f[8];
+        widen<DT>(v[j], f);
+        pack_chunk<DT, FMT>(f, at[j].c, a.packed + at[j].i * per_row * 8, a.scales + at[j].i * (per_row / 4));
+    }
 }
 
 template <int DT, int FMT>
-__global__ __launch_bounds__(kThreads) void unpack_kernel(const PackArgs a, uint32_t slices) {
-    const int lane = threadIdx.x & 63;
-    const Slice s = slice_of(slices);
-    if (s.i >= a.M) return;
-    const int64_t blocks = (a.N + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK;
-    const int full = (int)(a.N >> 3), tail = (int)(a.N & 7);
-    uint16_t* row = a.x + s.i * a.ldx;
-    const uint8_t* packed = a.packed + s.i * blocks * FO_PACK_BLOCK;
-    const uint8_t* scales = a.scales + s.i * blocks;
+__global__ __launch_bounds__(kThreads) void unpack_kernel(const PackArgs a, uint32_t chunks, uint32_t per_row) {
+    const uint32_t first = blockIdx.x * (kThreads * kAhead) + threadIdx.x;
     u32x2_t code[kAhead];
     uint32_t scale[kAhead];
+    Chunk at[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-        const int c = s.c0 + 64 * j + lane;
-        if (c < full) {
-            code[j] = *reinterpret_cast<const u32x2_t*>(packed + 8 * (int64_t)c);
-            scale[j] = scales[c >> 2];
-        }
+        const uint32_t q = first + j * kThreads;
+        if (q >= chunks) continue;
+        // (the codes' rows have no gaps)
+        at[j] = chunk_of(a, q, per_row);
+        code[j] = *reinterpret_cast<const u32x2_t*>(a.packed + 8 * (int64_t)q);
+        scale[j] = a.scales[q >> 2];
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-        const int c = s.c0 + 64 * j + lane;
-        if (c < full) {
-            float f[8];
-            decode8<FMT>(code[j], scale_of(scale[j]), f);
-            stream8(row + 8 * (int64_t)c, narrow<DT>(f));
+        if (first + j * kThreads >= chunks) continue;
+        const int64_t n = 8 * (int64_t)at[j].c;
+        uint16_t* to = a.x + at[j].i * a.ldx + n;
+        float f[8];
+        decode8<FMT>(code[j], scale_of(scale[j]), f);
+        const u32x4_t v = narrow<DT>(f);
+        if (n + 8 <= a.N) {
+            stream8(to, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 7; ++e)
+                if (n + e < a.N) to[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
         }
-    }
-    if (s.last && lane < tail) {
-        const int64_t n = a.N - tail + lane;
-        row[n] = (uint16_t)from_f32<DT>(decode1<FMT>(packed[n], scale_of(scales[n / FO_PACK_BLOCK])));
     }
 }
 
-uint32_t slices_of(int64_t N) { return (uint32_t)(N / 8 > kSlice ? (N / 8 + kSlice - 1) / kSlice : 1); }
-
-uint32_t workgroups(const PackArgs& a) { return (uint32_t)((a.M * slices_of(a.N) + kThreads / 64 - 1) / (kThreads / 64)); }
+using Kernel = void (*)(PackArgs, uint32_t, uint32_t);
+hipError_t launch_chunks(Kernel kernel, PackArgs a, hipStream_t s) {
+    if (a.ldx == a.N && a.N % FO_PACK_BLOCK == 0) {
+        a.N *= a.M;
+        a.ldx = a.N;
+        a.M = 1;
+    }
+    const int64_t per_row = 4 * pack_blocks(a.N), chunks = a.M * per_row;
+    return launch(kernel, (uint32_t)((chunks + kThreads * kAhead - 1) / (kThreads * kAhead)), kThreads, s, a,
+                  (uint32_t)chunks, (uint32_t)per_row);
+}
 
 }  // namespace
 
 hipError_t launch_pack(int dtype, int format, const PackArgs& a, hipStream_t s) {
     const bool int8 = format == FO_PACK_INT8;
-    return launch(dtype == FO_FP16 ? (int8 ? pack_kernel<FO_FP16, FO_PACK_INT8> : pack_kernel<FO_FP16, FO_PACK_E4M3>)
-                                   : (int8 ? pack_kernel<FO_BF16, FO_PACK_INT8> : pack_kernel<FO_BF16, FO_PACK_E4M3>),
-                  workgroups(a), kThreads, s, a, slices_of(a.N));
+    return launch_chunks(dtype == FO_FP16
+                             ? (int8 ? pack_kernel<FO_FP16, FO_PACK_INT8> : pack_kernel<FO_FP16, FO_PACK_E4M3>)
+                             : (int8 ? pack_kernel<FO_BF16, FO_PACK_INT8> : pack_kernel<FO_BF16, FO_PACK_E4M3>), a, s);
 }
 
 hipError_t launch_unpack(int dtype, int format, const PackArgs& a, hipStream_t s) {
     const bool int8 = format == FO_PACK_INT8;
-    return launch(dtype == FO_FP16 ? (int8 ? unpack_kernel<FO_FP16, FO_PACK_INT8> : unpack_kernel<FO_FP16, FO_PACK_E4M3>)
-                                   : (int8 ? unpack_kernel<FO_BF16, FO_PACK_INT8> : unpack_kernel<FO_BF16, FO_PACK_E4M3>),
-                  workgroups(a), kThreads, s, a, slices_of(a.N));
+    return launch_chunks(dtype == FO_FP16
+                             ? (int8 ? unpack_kernel<FO_FP16, FO_PACK_INT8> : unpack_kernel<FO_FP16, FO_PACK_E4M3>)
+                             : (int8 ? unpack_kernel<FO_BF16, FO_PACK_INT8> : unpack_kernel<FO_BF16, FO_PACK_E4M3>), a, s);
 }
 
 }  // namespace fo

@@ -184,8 +184,8 @@ static fo_status pack_args(int32_t dtype, int32_t format, int64_t M, int64_t N, 
     if (M == 0 || N == 0) return FO_OK;
     if ((st = fo::check_rows("x", x, N, ldx)) != FO_OK || (st = fo::check_pack(packed, scales, format)) != FO_OK)
         return st;
-    if (N > INT32_MAX || M > INT32_MAX || !fo::launchable((M * fo::slices_of(N) + 3) / 4, 256))
-        return fo::fail(FO_ERR_SHAPE, "too many rows or columns for one launch");
+    if (N > INT32_MAX || M > INT32_MAX || M * 4 * fo::pack_blocks(N) > (int64_t)UINT32_MAX - 1024)
+        return fo::fail(FO_ERR_SHAPE, "too many values for one launch");
     a->x = static_cast<uint16_t*>(const_cast<void*>(x));
     a->packed = static_cast<uint8_t*>(const_cast<void*>(packed));
     a->scales = static_cast<uint8_t*>(const_cast<void*>(scales));

@@ -229,7 +229,7 @@ __device__ __forceinline__ void decode8(u32x2_t code, float scale, float* f) {
 // A lane's chunk f of a whole block, packed with the three neighbours' that share it
 // (lanes 4 i .. 4 i + 3 hold chunks 4 j .. 4 j + 3; all four lanes call).
 template <int DT, int FMT>
-__device__ __forceinline__ void pack_chunk(const float* f, int c, uint8_t* packed_row, uint8_t* scale_row) {
+__device__ __forceinline__ void pack_chunk(const float* f, uint32_t c, uint8_t* packed_row, uint8_t* scale_row) {
     float top = top_of(f);
     // the other three lanes': quad_perm [1, 0, 3, 2], then [2, 3, 0, 1]
     top = __builtin_elementwise_maximum(
