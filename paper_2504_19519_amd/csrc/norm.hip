@@ -42,14 +42,17 @@ __device__ __forceinline__ int row_group() {
 // has several waves each takes the mean of its own values and the sum of their
 // squared differences from it, and one meeting joins them:
 //   sum of (x - mu)^2 = sum over waves of (their sum + n_w (mu_w - mu)^2).
-// Rows of up to half a wave share waves (a checkpoint's last block then has to be whole).
+// Rows of up to half a wave share waves.
 template <int DT, int CH, int TH, int ROWS>
 __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs a) {
     constexpr int kRowWaves = TH / 64;              // 0: several rows in a wave
     __shared__ float s_sum[2][2][TH * ROWS / 64];
     const int lane = threadIdx.x % TH, group = row_group<TH>();
     const int full = (int)(a.N >> 3), tail = (int)(a.N & 7);
-    const bool has_tail = lane < tail;
+    // The values behind the row's last whole chunk, fewer than eight: one to a lane, in
+    // the wave that packs them.
+    const int end_lane = TH <= 64 ? lane : lane - full % TH / 64 * 64;
+    const bool has_tail = end_lane >= 0 && end_lane < tail;
     const int64_t blocks = (a.N + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK, step = (int64_t)gridDim.x * ROWS;
     // A lane's sum is scaled by the power of two that makes N at most 1, so that the
     // row's sums (of squares: up to 2^120 on average) stay in fp32's range.
@@ -77,8 +80,8 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
             count += 8.0f;
         }
     }
-    if (a.gamma && has_tail) gamma_t = to_f32<DT>(a.gamma[8 * full + lane]);
-    if (a.beta && has_tail) beta_t = to_f32<DT>(a.beta[8 * full + lane]);
+    if (a.gamma && has_tail) gamma_t = to_f32<DT>(a.gamma[8 * full + end_lane]);
+    if (a.beta && has_tail) beta_t = to_f32<DT>(a.beta[8 * full + end_lane]);
     count = wave_sum(count * scale);                // of this wave, scaled like the sums (kRowWaves > 1)
     const float inv_count = count > 0.0f ? 1.0f / count : 0.0f;
     float wave_count = 0.0f;                        // lane w: of the row's wave w
@@ -97,7 +100,7 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
             v[t] = u32x4_t{0u, 0u, 0u, 0u};
             if (i < a.M && c < full) v[t] = load8(row + 8 * c);
         }
-        vt = i < a.M && has_tail ? row[8 * full + lane] : 0u;
+        vt = i < a.M && has_tail ? row[8 * full + end_lane] : 0u;
     };
 
     int64_t i = (int64_t)blockIdx.x * ROWS + group;
@@ -115,20 +118,30 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
         if (a.packed && i < a.M) {
             uint8_t* packed = a.packed + i * blocks * FO_PACK_BLOCK;
             uint8_t* scales = a.scales + i * blocks;
-            const int whole = (int)(a.N / FO_PACK_BLOCK) * 4;
+            // the values behind the last whole chunk, to the thread that packs them
+            float end[8] = {};
+            if (tail) {
+                const int from = TH < 64 ? (threadIdx.x & 63) - lane : 0;
+#pragma unroll
+                for (int e = 0; e < 7; ++e) {
+                    const float v = __shfl(xt, from + e, 64);
+                    end[e] = e < tail ? v : 0.0f;
+                }
+            }
 #pragma unroll
             for (int t = 0; t < CH; ++t) {
                 const int c = lane + TH * t;
-                if (c < whole) {
-                    if (a.format == FO_PACK_INT8) pack_chunk<DT, FO_PACK_INT8>(x[t], c, packed, scales);
-                    else pack_chunk<DT, FO_PACK_E4M3>(x[t], c, packed, scales);
+                float f[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = x[t][e];
+                if (tail && c == full) {
+#pragma unroll
+                    for (int e = 0; e < 7; ++e) f[e] = end[e];
                 }
-            }
-            // (read again here, ahead of any store to y, which may be x)
-            if (TH >= 64 && a.N % FO_PACK_BLOCK && lane < 64) {
-                const uint16_t* row = a.x + i * a.ldx;
-                if (a.format == FO_PACK_INT8) pack_last<DT, FO_PACK_INT8>(row, a.N, lane, packed, scales);
-                else pack_last<DT, FO_PACK_E4M3>(row, a.N, lane, packed, scales);
+                if (c < 4 * (int)blocks) {
+                    if (a.format == FO_PACK_INT8) pack_chunk<DT, FO_PACK_INT8>(f, c, packed, scales);
+                    else pack_chunk<DT, FO_PACK_E4M3>(f, c, packed, scales);
+                }
             }
         }
 
@@ -183,7 +196,7 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
             for (int e = 0; e < 8; ++e) g[e] = (x[t][e] - mean) * rstd * g[e] + b[e];
             if (c < full) stream8(out + 8 * c, narrow<DT>(g));
         }
-        if (has_tail) out[8 * full + lane] = (uint16_t)from_f32<DT>((xt - mean) * rstd * gamma_t + beta_t);
+        if (has_tail) out[8 * full + end_lane] = (uint16_t)from_f32<DT>((xt - mean) * rstd * gamma_t + beta_t);
     }
 }
 
@@ -486,11 +499,9 @@ void set_rows(NormForm& f, int64_t M, int threads, int64_t units) {
 // second; registers held down to two of 16 waves 69 and 83; a workgroup per row and
 // nothing ahead 60 and 61). Past 8192 columns, where a row has 16 waves and they fit
 // once: one (1280x12288 18.9; 22.8 with three, two of them waiting).
-NormForm norm_forward_form(int64_t M, int64_t N, bool pack) {
-    const bool share = !pack || N % FO_PACK_BLOCK == 0;
+NormForm norm_forward_form(int64_t M, int64_t N) {
     NormForm f{};
-    f.threads = share && N <= 512 ? (N <= 128 ? 8 : N <= 256 ? 16 : 32)
-              : N <= 1024 ? 64 : N <= 2048 ? 128 : N <= 4096 ? 256 : N <= 8192 ? 512 : 1024;
+    f.threads = N <= 128 ? 8 : N <= 256 ? 16 : N <= 512 ? 32 : N <= 1024 ? 64 : N <= 2048 ? 128 : N <= 4096 ? 256 : N <= 8192 ? 512 : 1024;
     f.chunks = N <= 16384 ? 2 : 4;
     set_rows(f, M, 512, N <= 8192 ? 768 : 256);
     return f;
@@ -510,7 +521,7 @@ NormForm norm_backward_form(int64_t M, int64_t N) {
 }
 
 hipError_t launch_norm_forward(int dtype, const NormArgs& a, hipStream_t s) {
-    const NormForm f = norm_forward_form(a.M, a.N, a.packed != nullptr);
+    const NormForm f = norm_forward_form(a.M, a.N);
     return for_forward(f, [&](auto ch, auto th, auto rows) {
         constexpr int CH = decltype(ch)::value, TH = decltype(th)::value, ROWS = decltype(rows)::value;
         return launch(dtype == FO_FP16 ? norm_forward_kernel<FO_FP16, CH, TH, ROWS>

@@ -40,19 +40,10 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const PackArgs a, uint32
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
         const uint32_t q = first + j * kThreads;
-        v[j] = u32x4_t{0u, 0u, 0u, 0u};
         if (q >= chunks) continue;
         at[j] = chunk_of(a, q, per_row);
         const int64_t n = 8 * (int64_t)at[j].c;
-        const uint16_t* from = a.x + at[j].i * a.ldx + n;
-        if (n + 8 <= a.N) {
-            v[j] = stream_load8(from);
-        } else {
-            // the row's end: what is left of it, then zeros
-#pragma unroll
-            for (int e = 0; e < 7; ++e)
-                if (n + e < a.N) v[j][e >> 1] |= (uint32_t)from[e] << (16 * (e & 1));
-        }
+        v[j] = read_chunk<kStreamed>(a.x + at[j].i * a.ldx + n, a.N - n);
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
@@ -82,17 +73,9 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(const PackArgs a, uint
     for (int j = 0; j < kAhead; ++j) {
         if (first + j * kThreads >= chunks) continue;
         const int64_t n = 8 * (int64_t)at[j].c;
-        uint16_t* to = a.x + at[j].i * a.ldx + n;
         float f[8];
         decode8<FMT>(code[j], scale_of(scale[j]), f);
-        const u32x4_t v = narrow<DT>(f);
-        if (n + 8 <= a.N) {
-            stream8(to, v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 7; ++e)
-                if (n + e < a.N) to[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
-        }
+        write_chunk(a.x + at[j].i * a.ldx + n, narrow<DT>(f), a.N - n);
     }
 }
 

@@ -190,11 +190,9 @@ __device__ __forceinline__ void zero_padding(const RouteArgs& a, uint16_t* rows,
     int32_t from = a.offsets[e] + a.counts[e], to = a.offsets[e + 1];
     from = from < 0 ? 0 : from;
     to = to > a.capacity ? a.capacity : to;
-    const int full = (int)(a.H >> 3), tail = (int)(a.H & 7);
     for (int64_t r = (int64_t)from + wave; r < to; r += per * waves) {
         uint16_t* row = rows + r * ld;
-        for (int c = lane; c < full; c += 64) stream8(row + 8 * (int64_t)c, u32x4_t{0u, 0u, 0u, 0u});
-        if (lane < tail) row[8 * (int64_t)full + lane] = 0;
+        for (int64_t h = 8 * lane; h < a.H; h += 512) write_chunk(row + h, u32x4_t{0u, 0u, 0u, 0u}, a.H - h);
     }
 }
 
@@ -204,19 +202,11 @@ __global__ __launch_bounds__(kThreads) void permute_kernel(const RouteArgs a, ui
     if (blockIdx.x >= blocks) return zero_padding(a, a.rows, a.ldr, blockIdx.x - blocks, per);
     const Unit u = unit_of(slices);
     if (u.t >= a.T) return;
-    const int lane = threadIdx.x & 63, full = (int)(a.H >> 3), tail = (int)(a.H & 7), c = u.s * 64 + lane;
-    const uint16_t* row = a.x + u.t * a.ldx;
-    const bool has_tail = u.s == (int)slices - 1 && lane < tail;
-    u32x4_t v{};
-    uint16_t vt = 0;
-    if (c < full) v = load8(row + 8 * (int64_t)c);
-    if (has_tail) vt = row[8 * (int64_t)full + lane];
+    const int64_t h = ((int64_t)u.s * 64 + (threadIdx.x & 63)) * 8, left = a.H - h;
+    const u32x4_t v = read_chunk<kCached>(a.x + u.t * a.ldx + h, left);
     for (int k = 0; k < a.K; ++k) {
         const int32_t slot = a.slot_of[(int64_t)u.t * a.K + k];
-        if (!is_row(a, slot)) continue;
-        uint16_t* out = a.rows + slot * a.ldr;
-        if (c < full) stream8(out + 8 * (int64_t)c, v);
-        if (has_tail) out[8 * (int64_t)full + lane] = vt;
+        if (is_row(a, slot)) write_chunk(a.rows + slot * a.ldr + h, v, left);
     }
 }
 
@@ -226,15 +216,14 @@ template <int DT, int FMT>
 __global__ __launch_bounds__(kThreads) void combine_kernel(const RouteArgs a, uint32_t slices) {
     const Unit u = unit_of(slices);
     if (u.t >= a.T) return;
-    const int lane = threadIdx.x & 63, full = (int)(a.H >> 3), tail = (int)(a.H & 7), c = u.s * 64 + lane;
-    const bool last = u.s == (int)slices - 1, has_tail = last && lane < tail;
+    const int c = u.s * 64 + (threadIdx.x & 63);
+    const int64_t h = 8 * (int64_t)c, left = a.H - h;
     const int64_t blocks = (a.H + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK, first = (int64_t)u.t * a.K;
-    float sum[8] = {}, sum_t = 0.0f;
+    float sum[8] = {};
     for (int k0 = 0; k0 < a.K; k0 += kBatch) {
         int32_t slot[kBatch];
         float w[kBatch];
         u32x4_t v[kBatch];
-        uint32_t vt[kBatch];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             slot[j] = k0 + j < a.K ? a.slot_of[first + k0 + j] : -1;
@@ -243,12 +232,7 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(const RouteArgs a, ui
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             v[j] = u32x4_t{0u, 0u, 0u, 0u};
-            vt[j] = 0u;
-            if (is_row(a, slot[j])) {
-                const uint16_t* row = a.rows + slot[j] * a.ldr;
-                if (c < full) v[j] = stream_load8(row + 8 * (int64_t)c);
-                if (has_tail) vt[j] = row[8 * (int64_t)full + lane];
-            }
+            if (is_row(a, slot[j])) v[j] = read_chunk<kStreamed>(a.rows + slot[j] * a.ldr + h, left);
         }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
@@ -257,19 +241,13 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(const RouteArgs a, ui
             widen<DT>(v[j], f);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += w[j] * f[e];
-            sum_t += w[j] * to_f32<DT>(vt[j]);
             if constexpr (FMT >= 0) {
-                uint8_t* packed = a.packed + slot[j] * blocks * FO_PACK_BLOCK;
-                uint8_t* scales = a.scales + slot[j] * blocks;
-                if (c < a.H / FO_PACK_BLOCK * 4) pack_chunk<DT, FMT>(f, c, packed, scales);
-                if (last && a.H % FO_PACK_BLOCK)
-                    pack_last<DT, FMT>(a.rows + slot[j] * a.ldr, a.H, lane, packed, scales);
+                if (c < 4 * blocks)
+                    pack_chunk<DT, FMT>(f, c, a.packed + slot[j] * blocks * FO_PACK_BLOCK, a.scales + slot[j] * blocks);
             }
         }
     }
-    uint16_t* out = a.out + u.t * a.ldo;
-    if (c < full) stream8(out + 8 * (int64_t)c, narrow<DT>(sum));
-    if (has_tail) out[8 * (int64_t)full + lane] = (uint16_t)from_f32<DT>(sum_t);
+    write_chunk(a.out + u.t * a.ldo + h, narrow<DT>(sum), left);
 }
 
 // WAVES waves per pair, each along its row: drows[slot] = w dout[t] and dw =
@@ -284,7 +262,7 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const RouteA
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t p = (int64_t)blockIdx.x * (kWaves / WAVES) + wave / WAVES;
     if (p >= (int64_t)a.T * a.K) return;
-    const int lane = threadIdx.x % kLanes, full = (int)(a.H >> 3), tail = (int)(a.H & 7);
+    const int lane = threadIdx.x % kLanes;
     const int32_t slot = a.slot_of[p];
     if (!is_row(a, slot)) {
         if (lane == 0 && a.dweights) a.dweights[p] = 0.0f;
@@ -298,30 +276,22 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const RouteA
     const uint8_t* scales = SRC ? a.scales + slot * blocks32 : nullptr;
     uint16_t* out = a.out ? a.out + slot * a.ldo : nullptr;
     float dot = 0.0f;
-    for (int c = lane; c < full; c += kLanes) {
+    for (int64_t h = 8 * lane; h < a.H; h += 8 * kLanes) {
+        const int64_t left = a.H - h;
         float g[8];
-        widen<DT>(load8(grow + 8 * (int64_t)c), g);
+        widen<DT>(read_chunk<kCached>(grow + h, left), g);
         if (a.dweights) {
             float f[8];
-            if constexpr (SRC == 0) widen<DT>(stream_load8(row + 8 * (int64_t)c), f);
-            else decode8<SRC - 1>(*reinterpret_cast<const u32x2_t*>(packed + 8 * (int64_t)c), scale_of(scales[c >> 2]), f);
+            if constexpr (SRC == 0) widen<DT>(read_chunk<kStreamed>(row + h, left), f);
+            else decode8<SRC - 1>(*reinterpret_cast<const u32x2_t*>(packed + h), scale_of(scales[h / FO_PACK_BLOCK]), f);
 #pragma unroll
             for (int e = 0; e < 8; ++e) dot += g[e] * f[e];
         }
         if (out) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) g[e] *= w;
-            stream8(out + 8 * (int64_t)c, narrow<DT>(g));
+            write_chunk(out + h, narrow<DT>(g), left);
         }
-    }
-    if (lane < tail) {
-        const int64_t c = 8 * (int64_t)full + lane;
-        const float g = to_f32<DT>(grow[c]);
-        if (a.dweights) {
-            if constexpr (SRC == 0) dot += g * to_f32<DT>(row[c]);
-            else dot += g * decode1<SRC - 1>(packed[c], scale_of(scales[c / FO_PACK_BLOCK]));
-        }
-        if (out) out[c] = (uint16_t)from_f32<DT>(g * w);
     }
     if (a.dweights) {
         dot = wave_sum(dot);
@@ -336,7 +306,7 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const RouteA
     }
 }
 
-uint32_t slices_of(int64_t H) { return (uint32_t)std::max<int64_t>(1, (H / 8 + 63) / 64); }
+uint32_t slices_of(int64_t H) { return (uint32_t)((H + 511) / 512); }
 // Workgroups per expert that zero padding rows.
 int padding_blocks(const RouteArgs& a) { return a.offsets ? std::max(1, std::min(16, 256 / a.E)) : 0; }
 

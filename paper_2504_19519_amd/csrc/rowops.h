@@ -52,7 +52,7 @@ struct NormForm {
 constexpr int64_t kMaxNormCols = 32768;
 // Columns of the partial sums: whole chunks, so that every row of them is 16-byte aligned.
 FO_HD inline int64_t norm_partial_cols(int64_t N) { return (N + 7) / 8 * 8; }
-NormForm norm_forward_form(int64_t M, int64_t N, bool pack);
+NormForm norm_forward_form(int64_t M, int64_t N);
 NormForm norm_backward_form(int64_t M, int64_t N);
 hipError_t launch_norm_forward(int dtype, const NormArgs& a, hipStream_t s);
 // The sums over rows go to a.partial; then dgamma and dbeta (each or null) are their sums.

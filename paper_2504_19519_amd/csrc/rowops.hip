@@ -55,7 +55,7 @@ fo_status done(hipError_t e, const char* what) {
     return e == hipSuccess ? FO_OK : fail(FO_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
-int64_t slices_of(int64_t n) { return std::max<int64_t>(1, (n / 8 + 63) / 64); }
+int64_t slices_of(int64_t n) { return (n + 511) / 512; }
 
 int64_t norm_partial_bytes(int64_t M, int64_t N) {
     const NormForm f = norm_backward_form(M, N);

@@ -11,24 +11,48 @@
 namespace fo {
 
 // Eight 16-bit values at any 2-byte aligned address: one 16-byte access (global
-// memory takes unaligned ones), so rows of odd length or stride need no kernel
-// of their own. The values behind a row's last whole chunk (fewer than eight)
-// are taken one by a lane.
+// memory takes unaligned ones), so that rows of odd length or stride need no kernel
+// of their own.
 __device__ __forceinline__ u32x4_t load8(const uint16_t* p) {
     u32x4_t v;
     __builtin_memcpy(&v, p, sizeof(v));
     return v;
 }
-__device__ __forceinline__ void store8(uint16_t* p, u32x4_t v) { __builtin_memcpy(p, &v, sizeof(v)); }
-// The same past the caches' keeping (nontemporal): large outputs that this kernel
-// does not read again.
+// The same past the caches' keeping (nontemporal): inputs that are read once, and
+// large outputs that the kernel does not read again.
 typedef uint32_t u32x4_near_t __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ u32x4_t stream_load8(const uint16_t* p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4_near_t*>(p));
+}
+
 __device__ __forceinline__ void stream8(uint16_t* p, u32x4_t v) {
     __builtin_nontemporal_store(v, reinterpret_cast<u32x4_near_t*>(p));
 }
-// And inputs that are read once.
-__device__ __forceinline__ u32x4_t stream_load8(const uint16_t* p) {
-    return __builtin_nontemporal_load(reinterpret_cast<const u32x4_near_t*>(p));
+
+// A row's chunk of which `left` values lie within the row: all eight, or the row's
+// last few one by one (the rest reads as zeros), or none.
+enum Through { kCached, kStreamed };
+template <Through T>
+__device__ __forceinline__ u32x4_t read_chunk(const uint16_t* p, int64_t left) {
+    u32x4_t v = {0u, 0u, 0u, 0u};
+    if (left >= 8) {
+        v = T == kStreamed ? stream_load8(p) : load8(p);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < left) v[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+    }
+    return v;
+}
+// Written the same way, past the caches' keeping.
+__device__ __forceinline__ void write_chunk(uint16_t* p, u32x4_t v, int64_t left) {
+    if (left >= 8) {
+        stream8(p, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < left) p[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+    }
 }
 
 template <int DT>
@@ -226,8 +250,9 @@ __device__ __forceinline__ void decode8(u32x2_t code, float scale, float* f) {
     decode4<FMT>(code[1], scale, f + 4);
 }
 
-// A lane's chunk f of a whole block, packed with the three neighbours' that share it
-// (lanes 4 i .. 4 i + 3 hold chunks 4 j .. 4 j + 3; all four lanes call).
+// A lane's chunk f, packed with the three neighbours' that share its block (lanes
+// 4 i .. 4 i + 3 hold chunks 4 j .. 4 j + 3; all four lanes call). Values behind the
+// row's end are zeros.
 template <int DT, int FMT>
 __device__ __forceinline__ void pack_chunk(const float* f, uint32_t c, uint8_t* packed_row, uint8_t* scale_row) {
     float top = top_of(f);
@@ -242,24 +267,6 @@ __device__ __forceinline__ void pack_chunk(const float* f, uint32_t c, uint8_t* 
     code[1] = encode4<FMT>(f + 4, b);
     *reinterpret_cast<u32x2_t*>(packed_row + 8 * (int64_t)c) = code;
     if ((c & 3) == 0) scale_row[c >> 2] = (uint8_t)b.byte;
-}
-
-// The row's last block where N is no multiple of 32: one value per lane of the
-// first 32, codes behind the row's end 0.
-template <int DT, int FMT>
-__device__ __forceinline__ void pack_last(const uint16_t* row, int64_t N, int lane, uint8_t* packed_row,
-                                          uint8_t* scale_row) {
-    const int64_t block = N / FO_PACK_BLOCK, n = block * FO_PACK_BLOCK + lane;
-    const uint32_t bits = lane < FO_PACK_BLOCK && n < N ? row[n] : 0u;
-    float top = __builtin_fabsf(to_f32<DT>(bits));
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) top = __builtin_elementwise_maximum(top, __shfl_xor(top, off, 64));
-    if (lane < FO_PACK_BLOCK) {
-        const BlockScale b = block_scale<DT, FMT>(top);
-        const float f[4] = {to_f32<DT>(bits), 0.0f, 0.0f, 0.0f};
-        packed_row[n] = (uint8_t)encode4<FMT>(f, b);
-        if (lane == 0) scale_row[block] = (uint8_t)b.byte;
-    }
 }
 
 }  // namespace fo
