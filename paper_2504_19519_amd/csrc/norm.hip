@@ -494,16 +494,16 @@ void set_rows(NormForm& f, int64_t M, int threads, int64_t units) {
 
 }  // namespace
 
-// Forward: three workgroups of eight waves per compute unit (8192x8192 fp16 52 us,
-// 16384x4096 bf16 with a checkpoint 56; one of 16 waves, on more rows, 66 for the
-// second; registers held down to two of 16 waves 69 and 83; a workgroup per row and
-// nothing ahead 60 and 61). Past 8192 columns, where a row has 16 waves and they fit
-// once: one (1280x12288 18.9; 22.8 with three, two of them waiting).
+// Forward: two workgroups of eight waves per compute unit (8192x8192 fp16 49 us,
+// 16384x4096 bf16 with a checkpoint 55; three, which fit, 53 and 57; one of 16 waves, on
+// more rows, 66 for the second; registers held down to two of 16 waves 69 and 83; a
+// workgroup per row and nothing ahead 60 and 61). Past 8192 columns, where a row has
+// 16 waves and they fit once: one (1280x12288 18.9; 22.8 with three, two of them waiting).
 NormForm norm_forward_form(int64_t M, int64_t N) {
     NormForm f{};
     f.threads = N <= 128 ? 8 : N <= 256 ? 16 : N <= 512 ? 32 : N <= 1024 ? 64 : N <= 2048 ? 128 : N <= 4096 ? 256 : N <= 8192 ? 512 : 1024;
     f.chunks = N <= 16384 ? 2 : 4;
-    set_rows(f, M, 512, N <= 8192 ? 768 : 256);
+    set_rows(f, M, 512, N <= 8192 ? 512 : 256);
     return f;
 }
 
