@@ -559,7 +559,8 @@ fo_status fo_unpack_rows(int32_t dtype, int32_t format, int64_t M, int64_t N, co
  * gamma, beta: [N] of dtype, NULL = 1 and 0. mean, rstd: [M] fp32 outputs for the
  * backward pass, or NULL. packed and scales: a checkpoint of x for the backward
  * pass, written on the way (both or neither). y may be x (same ld); otherwise the
- * buffers must not overlap. Magnitudes up to 2^60 stay within fp32 on the way.
+ * buffers must not overlap. Magnitudes up to 2^60 stay within fp32 on the way, and
+ * differences from the mean of 2^-60 (below that an eps has to outweigh them).
  * Errors: FO_ERR_ARG, FO_ERR_UNSUPPORTED, FO_ERR_SHAPE, FO_ERR_HIP.
  */
 fo_status fo_norm_forward(int32_t kind, int32_t dtype, int64_t M, int64_t N, const void* x, int64_t ldx,

@@ -20,6 +20,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "rowops.h"
 #include "rows.h"
@@ -169,15 +170,18 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
     }
 }
 
-// A wave's (token, slice of 64 chunks) in a grid of T tokens of `slices`.
+// A thread's token and chunk in a grid of T tokens of `slices` times L chunks: L
+// lanes to a slice (64, or fewer where a row is shorter than a wave).
 struct Unit {
-    int32_t t, s;
+    int32_t t, c;
 };
+template <int L>
 __device__ __forceinline__ Unit unit_of(uint32_t slices) {
-    const uint32_t u = blockIdx.x * kWaves + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t group = threadIdx.x / L;
+    const uint32_t u = blockIdx.x * (kThreads / L) + (L < 64 ? group : (uint32_t)__builtin_amdgcn_readfirstlane(group));
     Unit r;
     r.t = (int32_t)(u / slices);
-    r.s = (int32_t)(u - (uint32_t)r.t * slices);
+    r.c = (int32_t)(u - (uint32_t)r.t * slices) * L + (int)(threadIdx.x % L);
     return r;
 }
 
@@ -198,11 +202,12 @@ __device__ __forceinline__ void zero_padding(const RouteArgs& a, uint16_t* rows,
 
 __device__ __forceinline__ bool is_row(const RouteArgs& a, int32_t slot) { return slot >= 0 && slot < a.capacity; }
 
+template <int L>
 __global__ __launch_bounds__(kThreads) void permute_kernel(const RouteArgs a, uint32_t slices, uint32_t blocks, int per) {
     if (blockIdx.x >= blocks) return zero_padding(a, a.rows, a.ldr, blockIdx.x - blocks, per);
-    const Unit u = unit_of(slices);
+    const Unit u = unit_of<L>(slices);
     if (u.t >= a.T) return;
-    const int64_t h = ((int64_t)u.s * 64 + (threadIdx.x & 63)) * 8, left = a.H - h;
+    const int64_t h = 8 * (int64_t)u.c, left = a.H - h;
     const u32x4_t v = read_chunk<kCached>(a.x + u.t * a.ldx + h, left);
     for (int k = 0; k < a.K; ++k) {
         const int32_t slot = a.slot_of[(int64_t)u.t * a.K + k];
@@ -212,12 +217,11 @@ __global__ __launch_bounds__(kThreads) void permute_kernel(const RouteArgs a, ui
 
 // FMT: -1, or the format of the checkpoint that the rows are packed into. kBatch of
 // a token's rows are in flight together.
-template <int DT, int FMT>
+template <int DT, int FMT, int L>
 __global__ __launch_bounds__(kThreads) void combine_kernel(const RouteArgs a, uint32_t slices) {
-    const Unit u = unit_of(slices);
+    const Unit u = unit_of<L>(slices);
     if (u.t >= a.T) return;
-    const int c = u.s * 64 + (threadIdx.x & 63);
-    const int64_t h = 8 * (int64_t)c, left = a.H - h;
+    const int64_t h = 8 * (int64_t)u.c, left = a.H - h;
     const int64_t blocks = (a.H + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK, first = (int64_t)u.t * a.K;
     float sum[8] = {};
     for (int k0 = 0; k0 < a.K; k0 += kBatch) {
@@ -242,27 +246,25 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(const RouteArgs a, ui
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += w[j] * f[e];
             if constexpr (FMT >= 0) {
-                if (c < 4 * blocks)
-                    pack_chunk<DT, FMT>(f, c, a.packed + slot[j] * blocks * FO_PACK_BLOCK, a.scales + slot[j] * blocks);
+                if (u.c < 4 * blocks)
+                    pack_chunk<DT, FMT>(f, u.c, a.packed + slot[j] * blocks * FO_PACK_BLOCK, a.scales + slot[j] * blocks);
             }
         }
     }
     write_chunk(a.out + u.t * a.ldo + h, narrow<DT>(sum), left);
 }
 
-// WAVES waves per pair, each along its row: drows[slot] = w dout[t] and dw =
-// <dout[t], rows[slot]>. SRC: where the rows come from: 0 themselves, 1 + format a
-// checkpoint of them.
-template <int DT, int SRC, int WAVES>
+// L lanes per pair along its row (fewer than a wave, a wave or the whole workgroup):
+// drows[slot] = w dout[t] and dw = <dout[t], rows[slot]>. SRC: where the rows come
+// from: 0 themselves, 1 + format a checkpoint of them.
+template <int DT, int SRC, int L>
 __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const RouteArgs a, uint32_t blocks, int per) {
-    static_assert(WAVES == 1 || WAVES == kWaves, "a workgroup's pair meets once");
-    constexpr int kLanes = 64 * WAVES;
+    static_assert(L <= 64 || L == kThreads, "a workgroup's pair meets once");
     __shared__ float s_dot[kWaves];
     if (blockIdx.x >= blocks) return zero_padding(a, a.out, a.ldo, blockIdx.x - blocks, per);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t p = (int64_t)blockIdx.x * (kWaves / WAVES) + wave / WAVES;
+    const int group = threadIdx.x / L, lane = threadIdx.x % L;
+    const int64_t p = (int64_t)blockIdx.x * (kThreads / L) + (L < 64 ? group : __builtin_amdgcn_readfirstlane(group));
     if (p >= (int64_t)a.T * a.K) return;
-    const int lane = threadIdx.x % kLanes;
     const int32_t slot = a.slot_of[p];
     if (!is_row(a, slot)) {
         if (lane == 0 && a.dweights) a.dweights[p] = 0.0f;
@@ -276,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const RouteA
     const uint8_t* scales = SRC ? a.scales + slot * blocks32 : nullptr;
     uint16_t* out = a.out ? a.out + slot * a.ldo : nullptr;
     float dot = 0.0f;
-    for (int64_t h = 8 * lane; h < a.H; h += 8 * kLanes) {
+    for (int64_t h = 8 * lane; h < a.H; h += 8 * L) {
         const int64_t left = a.H - h;
         float g[8];
         widen<DT>(read_chunk<kCached>(grow + h, left), g);
@@ -294,19 +296,42 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const RouteA
         }
     }
     if (a.dweights) {
-        dot = wave_sum(dot);
-        if constexpr (WAVES > 1) {
-            if ((threadIdx.x & 63) == 0) s_dot[wave] = dot;
+        dot = lanes_sum<(L < 64 ? L : 64)>(dot);
+        if constexpr (L > 64) {
+            if ((threadIdx.x & 63) == 0) s_dot[threadIdx.x >> 6] = dot;
             __syncthreads();
             dot = 0.0f;
 #pragma unroll
-            for (int v = 0; v < WAVES; ++v) dot += s_dot[v];
+            for (int v = 0; v < kWaves; ++v) dot += s_dot[v];
         }
         if (lane == 0) a.dweights[p] = dot;
     }
 }
 
-uint32_t slices_of(int64_t H) { return (uint32_t)((H + 511) / 512); }
+template <int N>
+using Int = std::integral_constant<int, N>;
+// Lanes to a slice of a row of H values: a wave, or the most whose last slice leaves at
+// most an eighth of the row's lanes idle; calls go(lanes) with them. (262144 tokens of
+// 64 values, eight choices, a wave -> 8 lanes: permute 158 -> 55 us, combine 175 -> 53,
+// its backward pass 631 -> 133; 29127 tokens of 576, two slices of a wave -> nine of 8
+// lanes: combine with a checkpoint 106 -> 81, backward 149 -> 116.)
+template <typename F>
+hipError_t for_lanes(int64_t H, F go) {
+    auto fits = [&](int64_t lanes) { return (H + 8 * lanes - 1) / (8 * lanes) * (8 * lanes) <= H + H / 8; };
+    if (fits(64)) return go(Int<64>());
+    if (fits(32)) return go(Int<32>());
+    if (fits(16)) return go(Int<16>());
+    return go(Int<8>());
+}
+// Slices of a row, and workgroups of a launch, with L lanes to a slice.
+template <int L>
+uint32_t slices_of(int64_t H) {
+    return (uint32_t)((H + 8 * L - 1) / (8 * L));
+}
+template <int L>
+uint32_t workgroups(const RouteArgs& a) {
+    return (uint32_t)(((int64_t)a.T * slices_of<L>(a.H) + kThreads / L - 1) / (kThreads / L));
+}
 // Workgroups per expert that zero padding rows.
 int padding_blocks(const RouteArgs& a) { return a.offsets ? std::max(1, std::min(16, 256 / a.E)) : 0; }
 
@@ -330,45 +355,50 @@ hipError_t launch_sort(const SortArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_permute(const RouteArgs& a, hipStream_t s) {
-    const uint32_t slices = slices_of(a.H);
-    const uint32_t blocks = (uint32_t)(((int64_t)a.T * slices + kWaves - 1) / kWaves);
     const int per = padding_blocks(a);
-    return launch(permute_kernel, blocks + (uint32_t)(per * a.E), kThreads, s, a, slices, blocks, per);
+    return for_lanes(a.H, [&](auto lanes) {
+        constexpr int L = decltype(lanes)::value;
+        const uint32_t blocks = workgroups<L>(a);
+        return launch(permute_kernel<L>, blocks + (uint32_t)(per * a.E), kThreads, s, a, slices_of<L>(a.H), blocks, per);
+    });
 }
 
 hipError_t launch_combine(int dtype, const RouteArgs& a, hipStream_t s) {
-    const uint32_t slices = slices_of(a.H);
-    const int kept = a.packed ? a.format : -1;
-    return launch(dtype == FO_FP16 ? (kept < 0                ? combine_kernel<FO_FP16, -1>
-                                      : kept == FO_PACK_INT8 ? combine_kernel<FO_FP16, FO_PACK_INT8>
-                                                             : combine_kernel<FO_FP16, FO_PACK_E4M3>)
-                                   : (kept < 0                ? combine_kernel<FO_BF16, -1>
-                                      : kept == FO_PACK_INT8 ? combine_kernel<FO_BF16, FO_PACK_INT8>
-                                                             : combine_kernel<FO_BF16, FO_PACK_E4M3>),
-                  (uint32_t)(((int64_t)a.T * slices + kWaves - 1) / kWaves), kThreads, s, a, slices);
-}
-
-template <int DT, int WAVES>
-static hipError_t launch_back(const RouteArgs& a, uint32_t blocks, hipStream_t s) {
-    const int per = a.out ? padding_blocks(a) : 0;
-    return launch(!a.packed                     ? combine_backward_kernel<DT, 0, WAVES>
-                  : a.format == FO_PACK_INT8 ? combine_backward_kernel<DT, 1 + FO_PACK_INT8, WAVES>
-                                             : combine_backward_kernel<DT, 1 + FO_PACK_E4M3, WAVES>,
-                  blocks + (uint32_t)(per * a.E), kThreads, s, a, blocks, per);
+    return for_lanes(a.H, [&](auto lanes) {
+        constexpr int L = decltype(lanes)::value;
+        auto from = [&](auto dt) {
+            constexpr int DT = decltype(dt)::value;
+            return launch(!a.packed                     ? combine_kernel<DT, -1, L>
+                          : a.format == FO_PACK_INT8 ? combine_kernel<DT, FO_PACK_INT8, L>
+                                                     : combine_kernel<DT, FO_PACK_E4M3, L>,
+                          workgroups<L>(a), kThreads, s, a, slices_of<L>(a.H));
+        };
+        return dtype == FO_FP16 ? from(Int<FO_FP16>()) : from(Int<FO_BF16>());
+    });
 }
 
 hipError_t launch_combine_backward(int dtype, const RouteArgs& a, hipStream_t s) {
+    const int64_t pairs = (int64_t)a.T * a.K;
+    const int per = a.out ? padding_blocks(a) : 0;
+    auto go = [&](auto lanes) {
+        constexpr int L = decltype(lanes)::value;
+        const uint32_t blocks = (uint32_t)((pairs + kThreads / L - 1) / (kThreads / L));
+        auto from = [&](auto dt) {
+            constexpr int DT = decltype(dt)::value;
+            return launch(!a.packed                     ? combine_backward_kernel<DT, 0, L>
+                          : a.format == FO_PACK_INT8 ? combine_backward_kernel<DT, 1 + FO_PACK_INT8, L>
+                                                     : combine_backward_kernel<DT, 1 + FO_PACK_E4M3, L>,
+                          blocks + (uint32_t)(per * a.E), kThreads, s, a, blocks, per);
+        };
+        return dtype == FO_FP16 ? from(Int<FO_FP16>()) : from(Int<FO_BF16>());
+    };
     // Four waves per pair while the pairs are too few to fill the device with one each
     // (us, one wave -> four, H 7168 from an int8 checkpoint: 128 pairs 11.4 -> 5.1, 1024
     // 12.6 -> 7.7, 2048 14.1 -> 12.6, 4096 17.5 -> 22.6, 8192 32.9 -> 42.8). A workgroup
     // per token with all of its rows in flight read dout once but wrote in more places
     // at a time: 8192 pairs of two choices 43 -> 58 to 66.
-    const int64_t pairs = (int64_t)a.T * a.K;
-    if (pairs <= 2048)
-        return dtype == FO_FP16 ? launch_back<FO_FP16, kWaves>(a, (uint32_t)pairs, s)
-                                : launch_back<FO_BF16, kWaves>(a, (uint32_t)pairs, s);
-    const uint32_t blocks = (uint32_t)((pairs + kWaves - 1) / kWaves);
-    return dtype == FO_FP16 ? launch_back<FO_FP16, 1>(a, blocks, s) : launch_back<FO_BF16, 1>(a, blocks, s);
+    if (pairs <= 2048 && a.H > 512) return go(Int<kThreads>());
+    return for_lanes(a.H, go);
 }
 
 }  // namespace fo

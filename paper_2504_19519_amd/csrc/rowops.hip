@@ -55,7 +55,8 @@ fo_status done(hipError_t e, const char* what) {
     return e == hipSuccess ? FO_OK : fail(FO_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
-int64_t slices_of(int64_t n) { return (n + 511) / 512; }
+// Eighths of a wave that a row takes, at most (route.hip).
+int64_t slices_of(int64_t n) { return (n + 63) / 64; }
 
 int64_t norm_partial_bytes(int64_t M, int64_t N) {
     const NormForm f = norm_backward_form(M, N);
@@ -72,7 +73,8 @@ fo_status check_route(int32_t dtype, int64_t T, int32_t K, int64_t H, const void
     if (T > 0 && !slot_of) return fail(FO_ERR_ARG, "slot_of is NULL");
     if (!aligned(slot_of, 4) || !aligned(weights, 4))
         return fail(FO_ERR_ARG, "slot_of and weights must be 4-byte aligned");
-    if (!launchable((T * std::max<int64_t>(slices_of(H), K) + 3) / 4 + 16 * FO_ROUTE_MAX_EXPERTS, 256))
+    if (T * slices_of(H) > (int64_t)UINT32_MAX - 64 ||
+        !launchable((T * std::max<int64_t>((H + 511) / 512 + 1, K) + 3) / 4 + 16 * FO_ROUTE_MAX_EXPERTS, 256))
         return fail(FO_ERR_SHAPE, "too many rows for one launch");
     return FO_OK;
 }

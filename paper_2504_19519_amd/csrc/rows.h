@@ -29,18 +29,26 @@ __device__ __forceinline__ void stream8(uint16_t* p, u32x4_t v) {
     __builtin_nontemporal_store(v, reinterpret_cast<u32x4_near_t*>(p));
 }
 
-// A row's chunk of which `left` values lie within the row: all eight, or the row's
-// last few one by one (the rest reads as zeros), or none.
+// A row's chunk of which `left` values lie within the row: all eight; the row's last
+// few, as four, two and one of them (the rest reads as zeros); or none.
 enum Through { kCached, kStreamed };
 template <Through T>
 __device__ __forceinline__ u32x4_t read_chunk(const uint16_t* p, int64_t left) {
     u32x4_t v = {0u, 0u, 0u, 0u};
     if (left >= 8) {
         v = T == kStreamed ? stream_load8(p) : load8(p);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 7; ++e)
-            if (e < left) v[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+    } else if (left > 0) {
+        const int n = (int)left;
+        u32x2_t four = {0u, 0u};
+        uint32_t two = 0u, one = 0u;
+        if (n & 4) __builtin_memcpy(&four, p, sizeof(four));
+        if (n & 2) __builtin_memcpy(&two, p + (n & 4), sizeof(two));
+        if (n & 1) one = p[n & 6];
+        const uint32_t next = n & 2 ? two : one, last = n & 2 ? one : 0u;      // behind the four
+        v[0] = n & 4 ? four[0] : next;
+        v[1] = n & 4 ? four[1] : last;
+        v[2] = n & 4 ? next : 0u;
+        v[3] = n & 4 ? last : 0u;
     }
     return v;
 }
@@ -48,10 +56,14 @@ __device__ __forceinline__ u32x4_t read_chunk(const uint16_t* p, int64_t left) {
 __device__ __forceinline__ void write_chunk(uint16_t* p, u32x4_t v, int64_t left) {
     if (left >= 8) {
         stream8(p, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 7; ++e)
-            if (e < left) p[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+    } else if (left > 0) {
+        const int n = (int)left;
+        const u32x2_t four = {v[0], v[1]};
+        const uint32_t next = n & 4 ? v[2] : v[0], last = n & 4 ? v[3] : v[1];
+        const uint16_t one = (uint16_t)(n & 2 ? last : next);
+        if (n & 4) __builtin_memcpy(p, &four, sizeof(four));
+        if (n & 2) __builtin_memcpy(p + (n & 4), &next, sizeof(next));
+        if (n & 1) p[n & 6] = one;
     }
 }
 
@@ -124,7 +136,7 @@ __device__ __forceinline__ void wave_sums(float& a, float& b) {
     a = bit_cast<float>(__builtin_amdgcn_readlane(bit_cast<int>(v), 31));
     b = bit_cast<float>(__builtin_amdgcn_readlane(bit_cast<int>(v), 63));
 }
-// Sum over the first W lanes (a power of two up to 16), the same in each lane.
+// Sum over the first W lanes (up to 16; the others up to 16 hold zeros), the same in each lane.
 template <int W>
 __device__ __forceinline__ float first_sum(float v) {
     if constexpr (W > 1) v = add_moved<0x111, 0xF>(v);
