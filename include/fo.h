@@ -575,9 +575,10 @@ fo_status fo_norm_forward(int32_t kind, int32_t dtype, int64_t M, int64_t N, con
  * x, or packed and scales (a checkpoint of x): one of the two. mean (layer norm)
  * and rstd as the forward pass gave them. dx [M, N] of dtype, dgamma and dbeta [N]
  * fp32: each may be NULL, not all. dx may be dy or x (same ld). dgamma and dbeta
- * are overwritten (zeros for M = 0) and need a workspace of
- * fo_norm_workspace_bytes(M, N) bytes, 16-byte aligned, that no other call uses
- * meanwhile (its contents do not matter; a graph keeps using it on replay).
+ * are overwritten (zeros for M = 0). They, and any gradient of rows of more than 16384
+ * columns, need a workspace of fo_norm_workspace_bytes(M, N) bytes, 16-byte aligned,
+ * that no other call uses meanwhile (its contents do not matter; a graph keeps using
+ * it on replay).
  */
 int64_t fo_norm_workspace_bytes(int64_t M, int64_t N);
 fo_status fo_norm_backward(int32_t kind, int32_t dtype, int64_t M, int64_t N, const void* dy, int64_t lddy,

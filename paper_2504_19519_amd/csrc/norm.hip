@@ -407,6 +407,127 @@ __global__ __launch_bounds__(TH * ROWS) void norm_backward_kernel(const NormArgs
     if (a.with_beta) add_up(dbeta, dbeta_t, partial + norm_partial_cols(a.N));
 }
 
+// Rows of more than kHeldCols columns: sixteen waves cannot hold a row and its columns'
+// sums (four chunks per thread spilled: 0.7 TB/s). Two launches instead, which read dy and
+// x twice: a workgroup per row for the row's two sums, then 256 threads per 2048 columns
+// (a chunk each, kept sums as above) that go down every kWideGroups-th row.
+constexpr int64_t kHeldCols = 16384;
+constexpr int kWideThreads = 256, kWideGroups = 64;
+
+// Chunk c of row i as it is read, and what it stands for: dy and x - mean.
+template <int SRC>
+struct WideChunk {
+    u32x4_t g, x;
+    u32x2_t code;
+    uint32_t scale;
+};
+template <int SRC>
+__device__ __forceinline__ WideChunk<SRC> wide_chunk(const NormArgs& a, int64_t i, int c) {
+    const int64_t left = a.N - 8 * (int64_t)c;
+    WideChunk<SRC> p;
+    p.g = read_chunk<kCached>(a.dy + i * a.ldy + 8 * c, left);
+    if constexpr (SRC == 0) {
+        p.x = read_chunk<kCached>(a.x + i * a.ldx + 8 * c, left);
+    } else {
+        const int64_t blocks = (a.N + FO_PACK_BLOCK - 1) / FO_PACK_BLOCK;
+        p.code = *reinterpret_cast<const u32x2_t*>(a.packed + i * blocks * FO_PACK_BLOCK + 8 * c);
+        p.scale = a.scales[i * blocks + (c >> 2)];
+    }
+    return p;
+}
+template <int DT, int SRC>
+__device__ __forceinline__ void wide_values(const WideChunk<SRC>& p, float mean, float* d, float* t) {
+    widen<DT>(p.g, d);
+    if constexpr (SRC == 0) widen<DT>(p.x, t);
+    else decode8<SRC - 1>(p.code, scale_of(p.scale), t);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] -= mean;
+}
+
+// dots[2 i] = rstd mean(g), dots[2 i + 1] = rstd^2 mean(g h) of row i.
+template <int DT, int SRC>
+__global__ __launch_bounds__(1024) void norm_wide_dots_kernel(const NormArgs a) {
+    __shared__ float s_sum[2][2][16];
+    const int chunks = (int)((a.N + 7) >> 3), wave = threadIdx.x >> 6, w = threadIdx.x & 63;
+    int set = 0;
+    for (int64_t i = blockIdx.x; i < a.M; i += gridDim.x, set ^= 1) {
+        const float mean = a.layer ? a.mean[i] : 0.0f, rstd = a.rstd[i];
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll 4
+        for (int c = threadIdx.x; c < chunks; c += 1024) {
+            float d[8], t[8], g[8];
+            wide_values<DT, SRC>(wide_chunk<SRC>(a, i, c), mean, d, t);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] = 1.0f;
+            if (a.gamma) widen<DT>(read_chunk<kCached>(a.gamma + 8 * c, a.N - 8 * (int64_t)c), g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                s1 += d[e] * g[e];
+                s2 += (d[e] * g[e]) * t[e];
+            }
+        }
+        wave_sums(s1, s2);
+        if (w == 0) {
+            s_sum[set][0][wave] = s1;
+            s_sum[set][1][wave] = s2;
+        }
+        __syncthreads();
+        s1 = first_sum<16>(w < 16 ? s_sum[set][0][w] : 0.0f);
+        s2 = first_sum<16>(w < 16 ? s_sum[set][1][w] : 0.0f);
+        if (threadIdx.x == 0) {
+            const float inv_n = 1.0f / (float)a.N;
+            a.dots[2 * i] = a.layer ? rstd * (s1 * inv_n) : 0.0f;
+            a.dots[2 * i + 1] = rstd * rstd * (rstd * s2 * inv_n);
+        }
+    }
+}
+
+template <int DT, int SRC>
+__global__ __launch_bounds__(kWideThreads) void norm_wide_columns_kernel(const NormArgs a) {
+    const int c = blockIdx.x * kWideThreads + threadIdx.x;
+    const int64_t left = a.N - 8 * (int64_t)c;
+    if (left <= 0) return;
+    float gamma[8], dgamma[8] = {}, dbeta[8] = {};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) gamma[e] = 1.0f;
+    if (a.gamma) widen<DT>(read_chunk<kCached>(a.gamma + 8 * c, left), gamma);
+    constexpr int kAhead = 4;           // rows whose loads are in flight together
+    for (int64_t i0 = blockIdx.y; i0 < a.M; i0 += kAhead * kWideGroups) {
+        WideChunk<SRC> p[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int64_t i = i0 + j * kWideGroups;
+            p[j] = wide_chunk<SRC>(a, i < a.M ? i : i0, c);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int64_t i = i0 + j * kWideGroups;
+            if (i >= a.M) break;
+            const float mean = a.layer ? a.mean[i] : 0.0f, rstd = a.rstd[i];
+            float d[8], t[8];
+            wide_values<DT, SRC>(p[j], mean, d, t);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                dgamma[e] += (d[e] * rstd) * t[e];
+                dbeta[e] += d[e];
+            }
+            if (a.dx) {
+                const float c1 = a.dots[2 * i], c2 = a.dots[2 * i + 1];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[e] = rstd * (d[e] * gamma[e]) - c1 - t[e] * c2;
+                write_chunk(a.dx + i * a.lddx + 8 * c, narrow<DT>(d), left);
+            }
+        }
+    }
+    if (!a.partial) return;
+    float* out = a.partial + (int64_t)blockIdx.y * 2 * norm_partial_cols(a.N) + 8 * c;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        out[e] = dgamma[e];
+        if (a.with_beta) out[norm_partial_cols(a.N) + e] = dbeta[e];
+    }
+}
+
 // dgamma and dbeta: the sums of `count` workgroups' sums (2 * cols each), 32 columns
 // per workgroup: 8 threads of four columns, 32 rows at a time.
 constexpr int kReduceThreads = 256, kReduceCols = 32;
@@ -475,8 +596,7 @@ hipError_t for_backward(const NormForm& f, F go) {
         case 512: return for_rows<1, 512, 2, 1, 2>(f, go);
         case 768: return for_rows<2, 768, 1, 1, 2>(f, go);
         default:
-            return f.chunks == 1 ? for_rows<1, 1024, 1, 1, 2>(f, go)
-                   : f.chunks == 2 ? for_rows<2, 1024, 1, 1, 2>(f, go) : for_rows<4, 1024, 1, 1, 2>(f, go);
+            return f.chunks == 1 ? for_rows<1, 1024, 1, 1, 2>(f, go) : for_rows<2, 1024, 1, 1, 2>(f, go);
     }
 }
 
@@ -513,10 +633,12 @@ NormForm norm_backward_form(int64_t M, int64_t N) {
     NormForm f{};
     f.threads = N <= 64 ? 8 : N <= 128 ? 16 : N <= 256 ? 32 : N <= 512 ? 64 : N <= 1024 ? 128 : N <= 2048 ? 256
               : N <= 4096 ? 512 : N <= 8192 ? 1024 : N <= 12288 ? 768 : 1024;
-    f.chunks = N <= 8192 ? 1 : N <= 16384 ? 2 : 4;
+    f.chunks = N <= 8192 ? 1 : 2;
     set_rows(f, M, 1024, 256);
+    if (N > kHeldCols) f.blocks = (uint32_t)std::min<int64_t>(M, kWideGroups);       // rows of partial sums
     return f;
 }
+int64_t norm_dots_bytes(int64_t M, int64_t N) { return N > kHeldCols ? 8 * M : 0; }
 
 hipError_t launch_norm_forward(int dtype, const NormArgs& a, hipStream_t s) {
     const NormForm f = norm_forward_form(a.M, a.N);
@@ -531,7 +653,19 @@ hipError_t launch_norm_forward(int dtype, const NormArgs& a, hipStream_t s) {
 hipError_t launch_norm_backward(int dtype, const NormArgs& a, float* dgamma, float* dbeta, hipStream_t s) {
     const NormForm f = norm_backward_form(a.M, a.N);
     hipError_t e = hipSuccess;
-    if (a.M > 0)
+    if (a.M > 0 && a.N > kHeldCols) {
+        auto from = [&](auto dt, auto src) {
+            constexpr int DT = decltype(dt)::value, SRC = decltype(src)::value;
+            if (a.dx) e = launch(norm_wide_dots_kernel<DT, SRC>, (uint32_t)std::min<int64_t>(a.M, 1024), 1024, s, a);
+            const uint32_t slabs = (uint32_t)((a.N + 8 * kWideThreads - 1) / (8 * kWideThreads));
+            return e == hipSuccess ? launch(norm_wide_columns_kernel<DT, SRC>, dim3(slabs, f.blocks), kWideThreads, s, a) : e;
+        };
+        auto any = [&](auto dt) {
+            return !a.packed                     ? from(dt, Int<0>())
+                   : a.format == FO_PACK_INT8 ? from(dt, Int<1 + FO_PACK_INT8>()) : from(dt, Int<1 + FO_PACK_E4M3>());
+        };
+        e = dtype == FO_FP16 ? any(Int<FO_FP16>()) : any(Int<FO_BF16>());
+    } else if (a.M > 0) {
         e = for_backward(f, [&](auto ch, auto th, auto rows) {
             constexpr int CH = decltype(ch)::value, TH = decltype(th)::value, ROWS = decltype(rows)::value;
             // rows ahead, as the registers of the workgroup's waves allow
@@ -546,6 +680,7 @@ hipError_t launch_norm_backward(int dtype, const NormArgs& a, float* dgamma, flo
             };
             return dtype == FO_FP16 ? from(Int<FO_FP16>()) : from(Int<FO_BF16>());
         });
+    }
     if (e == hipSuccess && (dgamma || dbeta)) {
         const int count = a.M > 0 ? (int)f.blocks : 0;
         const int64_t per = (norm_partial_cols(a.N) + kReduceCols - 1) / kReduceCols;

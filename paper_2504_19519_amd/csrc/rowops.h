@@ -35,6 +35,7 @@ struct NormArgs {
     uint8_t* packed;            // checkpoint, or null
     uint8_t* scales;
     float* partial;             // backward: [blocks][2][norm_partial_cols(N)] sums of dy * h and dy, or null
+    float* dots;                // backward, wide rows: [M][2] (norm_dots_bytes)
     int64_t M, N, ldx, ldy, lddx;
     float eps;
     float scale;                // forward: the largest power of two with N * scale <= 1
@@ -54,6 +55,8 @@ constexpr int64_t kMaxNormCols = 32768;
 FO_HD inline int64_t norm_partial_cols(int64_t N) { return (N + 7) / 8 * 8; }
 NormForm norm_forward_form(int64_t M, int64_t N);
 NormForm norm_backward_form(int64_t M, int64_t N);
+// Workspace of rows too wide to be held, behind the partial sums.
+int64_t norm_dots_bytes(int64_t M, int64_t N);
 hipError_t launch_norm_forward(int dtype, const NormArgs& a, hipStream_t s);
 // The sums over rows go to a.partial; then dgamma and dbeta (each or null) are their sums.
 hipError_t launch_norm_backward(int dtype, const NormArgs& a, float* dgamma, float* dbeta, hipStream_t s);

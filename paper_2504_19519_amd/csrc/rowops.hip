@@ -128,7 +128,8 @@ fo_status fo_norm_forward(int32_t kind, int32_t dtype, int64_t M, int64_t N, con
 }
 
 int64_t fo_norm_workspace_bytes(int64_t M, int64_t N) {
-    return M < 0 || N < 0 || N > fo::kMaxNormCols ? 0 : fo::norm_partial_bytes(M, N);
+    return M < 0 || N < 0 || M > INT32_MAX || N > fo::kMaxNormCols ? 0
+                                                                   : fo::norm_partial_bytes(M, N) + fo::norm_dots_bytes(M, N);
 }
 
 fo_status fo_norm_backward(int32_t kind, int32_t dtype, int64_t M, int64_t N, const void* dy, int64_t lddy,
@@ -157,7 +158,8 @@ fo_status fo_norm_backward(int32_t kind, int32_t dtype, int64_t M, int64_t N, co
         if (!rstd || (kind == FO_NORM_LAYER && !mean)) return fo::fail(FO_ERR_ARG, "the rows' statistics are missing");
         if (fo::clash(dx, lddx, dy, lddy, M, N, true) || fo::clash(dx, lddx, x, ldx, M, N, true))
             return fo::fail(FO_ERR_ARG, "dx overlaps dy or x without being it");
-        if (sums && (!workspace || !fo::aligned(workspace, 16) || workspace_bytes < fo::norm_partial_bytes(M, N)))
+        if ((sums || fo::norm_dots_bytes(M, N) > 0) &&
+            (!workspace || !fo::aligned(workspace, 16) || workspace_bytes < fo_norm_workspace_bytes(M, N)))
             return fo::fail(FO_ERR_ARG, "workspace: fo_norm_workspace_bytes(M, N) bytes, 16-byte aligned");
     }
     fo::NormArgs a{};
@@ -170,6 +172,8 @@ fo_status fo_norm_backward(int32_t kind, int32_t dtype, int64_t M, int64_t N, co
     a.packed = static_cast<uint8_t*>(const_cast<void*>(packed));
     a.scales = static_cast<uint8_t*>(const_cast<void*>(scales));
     a.partial = sums ? static_cast<float*>(workspace) : nullptr;
+    if (fo::norm_dots_bytes(M, N) > 0)
+        a.dots = reinterpret_cast<float*>(static_cast<char*>(workspace) + fo::norm_partial_bytes(M, N));
     a.M = M; a.N = N; a.ldx = ldx; a.ldy = lddy; a.lddx = lddx;
     a.layer = kind == FO_NORM_LAYER;
     a.format = format;

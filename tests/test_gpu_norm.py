@@ -182,7 +182,7 @@ def test_in_place(N):
         np.testing.assert_array_equal(y.bits(), y2.bits())
         dx, work = Mat(M, N, dtype), torch.empty(fo.norm_workspace_bytes(M, N), dtype=torch.uint8, device="cuda")
         src = None if kept else x.t
-        fo.norm_backward("layer", dy.t, src, gamma, mean, rstd, dx.t, None, None, M, N, dtype, **kept)
+        fo.norm_backward("layer", dy.t, src, gamma, mean, rstd, dx.t, None, None, M, N, dtype, work if N > 16384 else None, **kept)
         over = Mat(M, N, dtype, values=dy.t)
         fo.norm_backward("layer", over.t, src, gamma, mean, rstd, over.t, f32(N), None, M, N, dtype, work, **kept)
         np.testing.assert_array_equal(dx.bits(), over.bits())
@@ -209,6 +209,23 @@ def test_parts_of_the_gradient():
                          work if with_g or with_b else None)
         torch.cuda.synchronize()
         check_backward("rms", "none", x, dy, gamma, None, rstd, dx, dg, db, f"parts {with_dx}{with_g}{with_b}")
+
+
+def test_wide_rows_in_parts():
+    """Rows past 16384 columns: two launches, the first for dx alone."""
+    torch = torch_mod()
+    for M, N in ((1, 16385), (130, 20000), (70, 32768), (259, 16400)):
+        for dtype, fmt in (("bf16", "none"), ("fp16", "int8"), ("bf16", "e4m3")):
+            both("layer", M, N, dtype, fmt, 81, ld=N + 3, shift=1)
+        x, dy, gamma, beta = inputs(M, N, "bf16", 82)
+        mean, rstd = f32(M), f32(M)
+        fo.norm_forward("layer", x.t, gamma, beta, Mat(M, N, "bf16").t, M, N, "bf16", 1e-6, mean, rstd)
+        work = torch.empty(fo.norm_workspace_bytes(M, N), dtype=torch.uint8, device="cuda")
+        for with_dx, with_g, with_b in ((1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 0, 1)):
+            dx, dg, db = Mat(M, N, "bf16") if with_dx else None, f32(N) if with_g else None, f32(N) if with_b else None
+            fo.norm_backward("layer", dy.t, x.t, gamma, mean, rstd, dx.t if dx else None, dg, db, M, N, "bf16", work)
+            torch.cuda.synchronize()
+            check_backward("layer", "none", x, dy, gamma, mean, rstd, dx, dg, db, f"wide {M}x{N} {with_dx}{with_g}{with_b}")
 
 
 def test_no_rows():

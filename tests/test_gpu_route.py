@@ -205,6 +205,16 @@ def test_lengths(H):
         whole(9, 3, 5, H, 4, dtype, fmt, H + i)
 
 
+@pytest.mark.parametrize("H", [16, 56, 65, 72, 120, 128, 136, 200, 250, 256, 264, 300, 320, 448, 576, 700])
+def test_lanes(H):
+    """Slices of 8, 16, 32 and 64 lanes, full and ragged, few pairs and many."""
+    whole(30, 2, 3, H, 1, "bf16", "none", H)
+    whole(30, 2, 3, H, 8, "fp16", "e4m3", H + 1)
+    if H in (72, 250, 576):
+        whole(700, 3, 5, H, 4, "bf16", "int8", H + 2)
+        whole(700, 3, 5, H, 1, "fp16", "none", H + 3)
+
+
 @pytest.mark.parametrize("T,K,E,align", [(1, 1, 1, 1), (1, 8, 256, 1), (3, 1, 4, 64), (16, 2, 8, 64), (7, 64, 300, 1), (130, 5, 6, 16),
                                          (33, 9, 1024, 2), (257, 4, 3, 256), (12, 16, 16, 1), (20, 6, 60, 1)])
 def test_routings(T, K, E, align):
