@@ -13,13 +13,13 @@ bool is_dtype(int32_t d) { return d == FO_FP16 || d == FO_BF16; }
 bool is_format(int32_t f) { return f == FO_PACK_INT8 || f == FO_PACK_E4M3; }
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-// Whether M rows of N 16-bit values each, ld apart, share memory with another such
-// matrix other than by being the same one.
-bool clash(const void* p, int64_t ldp, const void* q, int64_t ldq, int64_t M, int64_t N, bool same_allowed) {
-    if (!p || !q || M == 0 || N == 0) return false;
-    if (p == q && (ldp == ldq || M == 1)) return !same_allowed;
+// Whether two matrices of 16-bit values, Mp and Mq rows of N, ldp and ldq apart, share
+// memory other than by being the same one (where that is allowed).
+bool clash(const void* p, int64_t Mp, int64_t ldp, const void* q, int64_t Mq, int64_t ldq, int64_t N, bool same_allowed) {
+    if (!p || !q || Mp == 0 || Mq == 0 || N == 0) return false;
+    if (same_allowed && p == q && (ldp == ldq || Mp == 1)) return false;
     const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
-    const uintptr_t xe = x + 2 * (uintptr_t)((M - 1) * ldp + N), ye = y + 2 * (uintptr_t)((M - 1) * ldq + N);
+    const uintptr_t xe = x + 2 * (uintptr_t)((Mp - 1) * ldp + N), ye = y + 2 * (uintptr_t)((Mq - 1) * ldq + N);
     if (xe <= y || ye <= x) return false;
     if (ldp != ldq) return true;
     // columns side by side in rows of one length
@@ -108,7 +108,7 @@ fo_status fo_norm_forward(int32_t kind, int32_t dtype, int64_t M, int64_t N, con
         ((packed || scales) && (st = fo::check_pack(packed, scales, format)) != FO_OK))
         return st;
     if (M > INT32_MAX) return fo::fail(FO_ERR_SHAPE, "2^31 rows or more");
-    if (fo::clash(x, ldx, y, ldy, M, N, true)) return fo::fail(FO_ERR_ARG, "y overlaps x without being x");
+    if (fo::clash(x, M, ldx, y, M, ldy, N, true)) return fo::fail(FO_ERR_ARG, "y overlaps x without being x");
     fo::NormArgs a{};
     a.x = static_cast<const uint16_t*>(x);
     a.gamma = static_cast<const uint16_t*>(gamma);
@@ -156,7 +156,7 @@ fo_status fo_norm_backward(int32_t kind, int32_t dtype, int64_t M, int64_t N, co
             (st = fo::check_vectors(gamma, nullptr, mean, rstd)) != FO_OK)
             return st;
         if (!rstd || (kind == FO_NORM_LAYER && !mean)) return fo::fail(FO_ERR_ARG, "the rows' statistics are missing");
-        if (fo::clash(dx, lddx, dy, lddy, M, N, true) || fo::clash(dx, lddx, x, ldx, M, N, true))
+        if (fo::clash(dx, M, lddx, dy, M, lddy, N, true) || fo::clash(dx, M, lddx, x, M, ldx, N, true))
             return fo::fail(FO_ERR_ARG, "dx overlaps dy or x without being it");
         if ((sums || fo::norm_dots_bytes(M, N) > 0) &&
             (!workspace || !fo::aligned(workspace, 16) || workspace_bytes < fo_norm_workspace_bytes(M, N)))
@@ -274,6 +274,7 @@ fo_status fo_route_permute(int32_t dtype, int64_t T, int32_t K, int64_t H, const
         return st;
     if (T == 0 || H == 0 || capacity == 0) return FO_OK;
     if ((st = fo::check_rows("x", x, H, ldx)) != FO_OK || (st = fo::check_rows("rows", rows, H, ldr)) != FO_OK) return st;
+    if (fo::clash(x, T, ldx, rows, capacity, ldr, H, false)) return fo::fail(FO_ERR_ARG, "rows overlaps x");
     fo::RouteArgs a{};
     a.x = static_cast<const uint16_t*>(x);
     a.rows = static_cast<uint16_t*>(rows);
@@ -296,6 +297,7 @@ fo_status fo_route_combine(int32_t dtype, int64_t T, int32_t K, int64_t H, const
         (st = fo::check_rows("out", out, H, ldo)) != FO_OK ||
         ((packed || scales) && (st = fo::check_pack(packed, scales, format)) != FO_OK))
         return st;
+    if (fo::clash(rows, capacity, ldr, out, T, ldo, H, false)) return fo::fail(FO_ERR_ARG, "out overlaps rows");
     fo::RouteArgs a{};
     a.rows = static_cast<uint16_t*>(const_cast<void*>(rows));
     a.out = static_cast<uint16_t*>(out);
@@ -329,8 +331,9 @@ fo_status fo_route_combine_backward(int32_t dtype, int64_t T, int32_t K, int64_t
                   (read && !rows && (st = fo::check_pack(packed, scales, format)) != FO_OK) ||
                   (drows && capacity > 0 && (st = fo::check_rows("drows", drows, H, lddr)) != FO_OK)))
         return st;
-    if (drows && rows && fo::clash(drows, lddr, rows, ldr, capacity, H, true))
+    if (fo::clash(drows, capacity, lddr, read ? rows : nullptr, capacity, ldr, H, true))
         return fo::fail(FO_ERR_ARG, "drows overlaps rows without being it");
+    if (fo::clash(drows, capacity, lddr, dout, T, lddo, H, false)) return fo::fail(FO_ERR_ARG, "drows overlaps dout");
     fo::RouteArgs a{};
     a.x = static_cast<const uint16_t*>(dout);
     a.rows = static_cast<uint16_t*>(const_cast<void*>(rows));

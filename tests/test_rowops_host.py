@@ -102,6 +102,11 @@ def test_route_refusals():
                     dict(offsets=P + 2, counts=P, E=8)):
             refused(ARG, f, **bad)
     refused(ARG, permute, x=None)
+    refused(ARG, permute, x=2 * P)
+    refused(ARG, permute, x=2 * P + 2 * 7 * 64)
+    refused(ARG, combine, out=P + 2 * 64)
+    refused(ARG, back, dout=4 * P)
+    refused(ARG, back, dout=4 * P, ldr=128, lddr=128, lddo=130)
     for bad in (dict(out=None), dict(weights=P + 2), dict(packed=P), dict(scales=P), dict(packed=P + 8, scales=P)):
         refused(ARG, combine, **bad)
     for bad in (dict(dout=None), dict(drows=None, dweights=None), dict(rows=None), dict(packed=P, scales=P),
