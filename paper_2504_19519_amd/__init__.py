@@ -698,7 +698,8 @@ def packed_bytes(M: int, N: int):
 
 
 def norm_workspace_bytes(M: int, N: int) -> int:
-    """fo_norm_workspace_bytes: what norm_backward needs for dgamma and dbeta."""
+    """fo_norm_workspace_bytes: what norm_backward needs for dgamma and dbeta, and for
+    any gradient of rows of more than 16384 columns."""
     return lib().fo_norm_workspace_bytes(M, N)
 
 
