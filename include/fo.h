@@ -602,7 +602,8 @@ fo_status fo_norm_backward(int32_t kind, int32_t dtype, int64_t M, int64_t N, co
  * case: T * K + min(E, T * K) * (align - 1)). K <= FO_ROUTE_MAX_CHOICES,
  * E <= FO_ROUTE_MAX_EXPERTS. workspace: fo_route_workspace_bytes(T, K, E) bytes
  * (0 for a few thousand pairs), 4-byte aligned, not shared with a concurrent call.
- * The same expert may be chosen twice by a token: each choice has a row.
+ * The same expert may be chosen twice by a token: each choice has a row. ids and
+ * the outputs must not overlap.
  */
 #define FO_ROUTE_MAX_CHOICES 64
 #define FO_ROUTE_MAX_EXPERTS 1024

@@ -580,7 +580,7 @@ hipError_t for_forward(const NormForm& f, F go) {
         case 64: return for_rows<2, 64, 8, 1, 2>(f, go);
         case 128: return for_rows<2, 128, 4, 1, 2>(f, go);
         case 256: return for_rows<2, 256, 2, 1, 2>(f, go);
-        case 512: return for_rows<2, 512, 1, 1, 2>(f, go);
+        case 512: return f.chunks == 2 ? for_rows<2, 512, 1, 1, 2>(f, go) : for_rows<3, 512, 1, 1, 2>(f, go);
         default: return f.chunks == 2 ? for_rows<2, 1024, 1, 1, 2>(f, go) : for_rows<4, 1024, 1, 1, 2>(f, go);
     }
 }
@@ -615,13 +615,17 @@ void set_rows(NormForm& f, int64_t M, int threads, int64_t units) {
 // Forward: two workgroups of eight waves per compute unit (8192x8192 fp16 49 us,
 // 16384x4096 bf16 with a checkpoint 55; three, which fit, 53 and 57; one of 16 waves, on
 // more rows, 66 for the second; registers held down to two of 16 waves 69 and 83; a
-// workgroup per row and nothing ahead 60 and 61). Past 8192 columns, where a row has
-// 16 waves and they fit once: one (1280x12288 18.9; 22.8 with three, two of them waiting).
+// workgroup per row and nothing ahead 60 and 61). Up to 12288 columns eight waves
+// take a row in three chunks, two workgroups per compute unit for fewer than 4096 rows
+// and one from there on (bf16, two against one, us: 1280x12288 10.9 and 12.0, with a
+// checkpoint 16.5 and 18.7; 4096x12288 37.0 and 36.8, 44.9 and 45.0; 16384x12288 149 and
+// 144, 178 and 162; 16 waves and two chunks 13.1, 18.6, 40.4, 46.3, 145 and 168). Past that a row has 16 waves and they fit once
+// (eight waves of four chunks: 16384x13000 with a checkpoint 190, 16 waves 181).
 NormForm norm_forward_form(int64_t M, int64_t N) {
     NormForm f{};
-    f.threads = N <= 128 ? 8 : N <= 256 ? 16 : N <= 512 ? 32 : N <= 1024 ? 64 : N <= 2048 ? 128 : N <= 4096 ? 256 : N <= 8192 ? 512 : 1024;
-    f.chunks = N <= 16384 ? 2 : 4;
-    set_rows(f, M, 512, N <= 8192 ? 512 : 256);
+    f.threads = N <= 128 ? 8 : N <= 256 ? 16 : N <= 512 ? 32 : N <= 1024 ? 64 : N <= 2048 ? 128 : N <= 4096 ? 256 : N <= 12288 ? 512 : 1024;
+    f.chunks = N <= 8192 ? 2 : N <= 12288 ? 3 : N <= 16384 ? 2 : 4;
+    set_rows(f, M, 512, N <= 8192 || (N <= 12288 && M < 4096) ? 512 : 256);
     return f;
 }
 

@@ -17,7 +17,9 @@ bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p
 // memory other than by being the same one (where that is allowed).
 bool clash(const void* p, int64_t Mp, int64_t ldp, const void* q, int64_t Mq, int64_t ldq, int64_t N, bool same_allowed) {
     if (!p || !q || Mp == 0 || Mq == 0 || N == 0) return false;
-    if (same_allowed && p == q && (ldp == ldq || Mp == 1)) return false;
+    if (Mp == 1) ldp = ldq;         // one row has no distance of its own
+    if (Mq == 1) ldq = ldp;
+    if (same_allowed && p == q && ldp == ldq) return false;
     const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
     const uintptr_t xe = x + 2 * (uintptr_t)((Mp - 1) * ldp + N), ye = y + 2 * (uintptr_t)((Mq - 1) * ldq + N);
     if (xe <= y || ye <= x) return false;

@@ -229,6 +229,26 @@ def test_strides_and_alignment(H, ldx, ldr, shift):
         whole(11, 2, 4, H, 8, "bf16", fmt, 5, ldx, ldr, shift)
 
 
+def test_one_token_beside_its_rows():
+    """One token whose values lie between two of the rows that they go to."""
+    torch = torch_mod()
+    say("[route] one token beside its rows")
+    H, K = 64, 2
+    block = torch.zeros(K, 2 * H, dtype=torch.bfloat16, device="cuda")
+    block[0, H:] = torch.arange(H, dtype=torch.bfloat16, device="cuda")
+    x, rows = block[:1, H:], block[:, :H]
+    slot = torch.tensor([1, 0], dtype=torch.int32, device="cuda")
+    fo.route_permute(x, slot, rows, 1, K, H, "bf16", K)
+    torch.cuda.synchronize()
+    assert torch.equal(rows, x.expand(K, H))
+    out = block[1:, H:]
+    fo.route_combine(rows, slot, None, out, 1, K, H, "bf16", K)
+    torch.cuda.synchronize()
+    assert torch.equal(out, 2 * x)              # even integers up to 126: exact
+    with pytest.raises(fo.FoError):
+        fo.route_combine(rows, slot, None, block[:1, H - 1:2 * H - 1], 1, K, H, "bf16", K)
+
+
 def test_slots_outside_the_rows_are_skipped():
     torch = torch_mod()
     T, K, H, cap = 4, 2, 64, 3
