@@ -70,7 +70,7 @@ struct PackArgs {
 hipError_t launch_pack(int dtype, int format, const PackArgs& a, hipStream_t s);
 hipError_t launch_unpack(int dtype, int format, const PackArgs& a, hipStream_t s);
 
-constexpr int kMaxExperts = 1024;
+constexpr int kMaxExperts = FO_ROUTE_MAX_EXPERTS;
 struct SortArgs {
     const void* ids;            // [pairs], of id_bytes each
     int64_t pairs;

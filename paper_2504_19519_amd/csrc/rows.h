@@ -18,8 +18,8 @@ __device__ __forceinline__ u32x4_t load8(const uint16_t* p) {
     __builtin_memcpy(&v, p, sizeof(v));
     return v;
 }
-// The same past the caches' keeping (nontemporal): inputs that are read once, and
-// large outputs that the kernel does not read again.
+// The same past the caches' keeping (nontemporal), for inputs that are read once and
+// outputs that the kernel does not read again.
 typedef uint32_t u32x4_near_t __attribute__((ext_vector_type(4), aligned(2)));
 __device__ __forceinline__ u32x4_t stream_load8(const uint16_t* p) {
     return __builtin_nontemporal_load(reinterpret_cast<const u32x4_near_t*>(p));
@@ -255,7 +255,7 @@ __device__ __forceinline__ float decode1(uint32_t code, float scale) {
     return f[0];
 }
 
-// Chunk c of a checkpoint's row (codes at `row`, scale bytes at `scale`).
+// What a chunk's eight codes stand for.
 template <int FMT>
 __device__ __forceinline__ void decode8(u32x2_t code, float scale, float* f) {
     decode4<FMT>(code[0], scale, f);
