@@ -39,7 +39,10 @@ __device__ __forceinline__ int row_group() {
 // beta, and the next row's loads are issued ahead of this row's sums. Where a row
 // has several waves each takes the mean of its own values and the sum of their
 // squared differences from it, and one meeting joins them:
+//   mu = mu_0 + sum over waves of n_w (mu_w - mu_0) / N,
 //   sum of (x - mu)^2 = sum over waves of (their sum + n_w (mu_w - mu)^2).
+// (The sum of the waves' n_w mu_w itself is rounded past 24 bits: rows of one fp16 value and more
+// than 8192 columns then had a mean one step off, 0.89 in y for values of 2^14 and an eps of 1e-6.)
 // Rows of up to half a wave share waves.
 template <int DT, int CH, int TH, int ROWS>
 __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs a) {
@@ -55,11 +58,12 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
     // A lane's sum is scaled by the power of two that makes N at most 1, so that the
     // row's sums (of squares: up to 2^120 on average) stay in fp32's range.
     const float scale = a.scale, n = (float)a.N * scale, inv_n = 1.0f / n;
-    // A sum's quotient by n: the error of the product with 1 / n is taken back, so that a
-    // row of one value has that value for its mean.
-    auto mean_of = [&](float sum) {
-        const float q = sum * inv_n;
-        return q + (sum - q * n) * inv_n;
+    // A sum's quotient by a count, the error of the product with its reciprocal taken back:
+    // a wave's sum of one 16-bit value, up to 2055 times, is exact, and so is that value as
+    // its mean.
+    auto quotient = [](float sum, float count, float inverse) {
+        const float q = sum * inverse;
+        return __builtin_fmaf(__builtin_fmaf(-q, count, sum), inverse, q);
     };
 
     u32x4_t gamma[CH], beta[CH];
@@ -151,7 +155,7 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum += x[t][e];
             sum = lanes_sum<(TH < 64 ? TH : 64)>(sum * scale);
-            mean = kRowWaves > 1 ? sum * inv_count : mean_of(sum);
+            mean = kRowWaves > 1 ? quotient(sum, count, inv_count) : quotient(sum, n, inv_n);
         }
 #pragma unroll
         for (int t = 0; t < CH; ++t) {
@@ -173,7 +177,8 @@ __global__ __launch_bounds__(TH * ROWS) void norm_forward_kernel(const NormArgs 
             const bool there = w < kRowWaves;
             const float mw = there ? s_sum[set][0][group * kRowWaves + w] : 0.0f;
             const float qw = there ? s_sum[set][1][group * kRowWaves + w] : 0.0f;
-            mean = a.layer ? mean_of(first_sum<kRowWaves>(mw * wave_count)) : 0.0f;
+            const float m0 = bit_cast<float>(__builtin_amdgcn_readfirstlane(bit_cast<int>(mw)));
+            mean = a.layer ? __builtin_fmaf(first_sum<kRowWaves>(wave_count * (mw - m0)), inv_n, m0) : 0.0f;
             square = first_sum<kRowWaves>(qw + wave_count * ((mw - mean) * (mw - mean)));
         }
         const float rstd = rsqrt_of(square * inv_n + a.eps);
