@@ -586,6 +586,17 @@ def _pick(table, key, what: str) -> int:
         raise ValueError(f"{what}: one of {[k for k in table if isinstance(k, str)]}, got {key!r}") from None
 
 
+def _holds_rows(shape, width: int) -> bool:
+    """Whether a row of `width` elements is a whole number of a contiguous tensor's last
+    dimensions; of other shapes a flat reading would cut the rows in the wrong places."""
+    n = 1
+    for k in reversed(shape):
+        n *= k
+        if n >= width:
+            break
+    return n == width
+
+
 _TYPES = {}          # element types that an argument takes, once a tensor has been seen
 
 
@@ -602,9 +613,10 @@ def _types():
 class _Args:
     """Pointers of one row operator's arguments. Tensors are checked: on one GPU,
     the current one (and the stream's), of the dtype that the call takes, large
-    enough, and contiguous or (matrices) with rows of unit stride. Raw pointers are
-    taken as given. (Written out for few Python calls per tensor: they are what a call
-    on a few rows takes.)"""
+    enough, and contiguous or (matrices) with rows of unit stride; one of several
+    dimensions has to hold the call's rows as they are (a one-dimensional one, or one
+    given with a row distance, is storage). Raw pointers are taken as given. (Written
+    out for few Python calls per tensor: they are what a call on a few rows takes.)"""
 
     __slots__ = ("dtype", "device", "stream")
 
@@ -646,14 +658,19 @@ class _Args:
                     raise ValueError(f"{what}: rows of unit stride that do not overlap are needed, strides are "
                                      f"{tuple(x.stride())}")
                 return x.data_ptr(), step if M > 1 else N
+        whole = ld is not None or M == 0 or N == 0 or x.dim() < 2 or _holds_rows(x.shape, N)
         ld = N if ld is None else int(ld)
         need = (M - 1) * ld + N if M > 0 and N > 0 else 0
+        if not whole:
+            raise ValueError(f"{what}: shape {tuple(x.shape)} for rows of {N}: a [{M}, {N}] view or a row distance "
+                             f"is needed")
         if not x.is_contiguous() or x.numel() < need:
             raise ValueError(f"{what}: {need} contiguous elements are needed, or a [{M}, {N}] view")
         return x.data_ptr(), ld
 
-    def flat(self, x, count: int, what: str, kind=None):
-        """Pointer of `count` contiguous elements of a kind (None: the values')."""
+    def flat(self, x, count: int, what: str, kind=None, width: int = 0):
+        """Pointer of `count` contiguous elements of a kind (None: the values'), in rows
+        of `width` (0: a vector)."""
         if x is None:
             return None
         try:
@@ -664,8 +681,11 @@ class _Args:
             self._place(d, what)
         if x.dtype not in (_TYPES or _types())[self.dtype if kind is None else kind]:
             raise ValueError(f"{what}: elements of {x.dtype}")
-        if x.numel() < count or not x.is_contiguous():
+        have = x.numel()
+        if have < count or not x.is_contiguous():
             raise ValueError(f"{what}: {count} contiguous elements are needed")
+        if width and have > count > 0 and x.dim() > 1 and not _holds_rows(x.shape, width):
+            raise ValueError(f"{what}: shape {tuple(x.shape)} for rows of {width}")
         return x.data_ptr()
 
     def space(self, x, what: str = "workspace"):
@@ -686,9 +706,9 @@ class _Args:
         """(packed, scales, format) of an [M, N] checkpoint."""
         if packed is None and scales is None:
             return None, None, 0
-        codes, steps = packed_bytes(M, N)
-        return (self.flat(packed, codes, "packed", "u8"), self.flat(scales, steps, "scales", "u8"),
-                _pick(_FORMATS, fmt, "fmt"))
+        blocks = -(-N // PACK_BLOCK)
+        return (self.flat(packed, M * blocks * PACK_BLOCK, "packed", "u8", blocks * PACK_BLOCK),
+                self.flat(scales, M * blocks, "scales", "u8", blocks), _pick(_FORMATS, fmt, "fmt"))
 
 
 def packed_bytes(M: int, N: int):
@@ -770,9 +790,9 @@ def route_sort(ids, T: int, K: int, E: int, offsets, counts, slot_of, pair_of=No
     rows = int(capacity) if capacity is not None else pair_of.numel() if hasattr(pair_of, "numel") else \
         route_capacity(T, K, E, align)
     work, nbytes = a.space(workspace)
-    _check(lib().fo_route_sort(a.flat(ids, T * K, "ids", "ids"), size, T, K, E, align,
+    _check(lib().fo_route_sort(a.flat(ids, T * K, "ids", "ids", K), size, T, K, E, align,
                                a.flat(offsets, E + 1, "offsets", "i32"), a.flat(counts, E, "counts", "i32"),
-                               a.flat(slot_of, T * K, "slot_of", "i32"), a.flat(pair_of, rows, "pair_of", "i32"),
+                               a.flat(slot_of, T * K, "slot_of", "i32", K), a.flat(pair_of, rows, "pair_of", "i32"),
                                rows, work, nbytes, _stream(stream)))
 
 
@@ -783,7 +803,7 @@ def route_permute(x, slot_of, rows, T: int, K: int, H: int, dtype, capacity: int
     a = _Args(dtype, stream)
     px, sx = a.rows(x, T, H, ldx, "x")
     pr, sr = a.rows(rows, capacity, H, ldr, "rows")
-    _check(lib().fo_route_permute(a.dtype, T, K, H, px, sx, a.flat(slot_of, T * K, "slot_of", "i32"), pr, sr,
+    _check(lib().fo_route_permute(a.dtype, T, K, H, px, sx, a.flat(slot_of, T * K, "slot_of", "i32", K), pr, sr,
                                   capacity, a.flat(offsets, E + 1, "offsets", "i32"),
                                   a.flat(counts, E, "counts", "i32"), E, _stream(stream)))
 
@@ -797,8 +817,8 @@ def route_combine(rows, slot_of, weights, out, T: int, K: int, H: int, dtype, ca
     pr, sr = a.rows(rows, capacity, H, ldr, "rows")
     po, so = a.rows(out, T, H, ldo, "out")
     codes, steps, fmt = a.pack(packed, scales, capacity, H, fmt)
-    _check(lib().fo_route_combine(a.dtype, T, K, H, pr, sr, capacity, a.flat(slot_of, T * K, "slot_of", "i32"),
-                                  a.flat(weights, T * K, "weights", "f32"), po, so, codes, steps, fmt,
+    _check(lib().fo_route_combine(a.dtype, T, K, H, pr, sr, capacity, a.flat(slot_of, T * K, "slot_of", "i32", K),
+                                  a.flat(weights, T * K, "weights", "f32", K), po, so, codes, steps, fmt,
                                   _stream(stream)))
 
 
@@ -814,8 +834,8 @@ def route_combine_backward(dout, rows, slot_of, weights, drows, dweights, T: int
     pd, sd = a.rows(drows, capacity, H, lddr, "drows")
     codes, steps, fmt = a.pack(packed, scales, capacity, H, fmt)
     _check(lib().fo_route_combine_backward(a.dtype, T, K, H, pg, sg, pr, sr, codes, steps, fmt, capacity,
-                                           a.flat(slot_of, T * K, "slot_of", "i32"),
-                                           a.flat(weights, T * K, "weights", "f32"), pd, sd,
-                                           a.flat(dweights, T * K, "dweights", "f32"),
+                                           a.flat(slot_of, T * K, "slot_of", "i32", K),
+                                           a.flat(weights, T * K, "weights", "f32", K), pd, sd,
+                                           a.flat(dweights, T * K, "dweights", "f32", K),
                                            a.flat(offsets, E + 1, "offsets", "i32"),
                                            a.flat(counts, E, "counts", "i32"), E, _stream(stream)))
