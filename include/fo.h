@@ -520,10 +520,12 @@ fo_status fo_run_overlapped_noalloc(const fo_plan* plan, const void* dev_plan,
  *
  * Matrices of 16-bit values (dtype: fo_dtype) are row-major with rows `ld`
  * elements apart (ld >= the row's length; 2-byte aligned, any length, odd ones
- * included). Sums are in fp32 and results are rounded once. One call is one or
- * two launches on `stream`, safe to capture; equal calls give equal bits. Sizes
- * of zero are accepted. FO_ERR_SHAPE: more rows than one launch takes (2^32
- * work-items).
+ * included). Sums are in fp32 and results are rounded once. One call is one to
+ * three launches on `stream` (three: the norm's backward pass of more than 16384
+ * columns), safe to capture; equal calls give equal bits. Sizes of zero are
+ * accepted. What a call writes must not overlap anything else that it reads or
+ * writes, unless its description says so. FO_ERR_SHAPE: more rows than one launch
+ * takes (2^32 work-items).
  */
 
 typedef enum { FO_NORM_LAYER = 0, FO_NORM_RMS = 1 } fo_norm;

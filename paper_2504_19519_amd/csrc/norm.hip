@@ -412,10 +412,12 @@ __global__ __launch_bounds__(TH * ROWS) void norm_backward_kernel(const NormArgs
     if (a.with_beta) add_up(dbeta, dbeta_t, partial + norm_partial_cols(a.N));
 }
 
-// Rows of more than kHeldCols columns: sixteen waves cannot hold a row and its columns'
-// sums (four chunks per thread spilled: 0.7 TB/s). Two launches instead, which read dy and
-// x twice: a workgroup per row for the row's two sums, then 256 threads per 2048 columns
-// (a chunk each, kept sums as above) that go down every kWideGroups-th row.
+// Rows of more than kHeldCols columns: the registers of sixteen waves cannot hold a row and
+// its columns' sums (four chunks per thread spilled: 0.7 TB/s; a row kept in LDS was not
+// tried). Two launches instead, which read dy and x twice: a workgroup per row for the row's
+// two sums, then 256 threads per 2048 columns (a chunk each, kept sums as above) that go
+// down every kWideGroups-th row. bf16, from x and from int8: 1024x32768 74 and 71 us with
+// the last launch (2.7 and 2.4 TB/s of what the gradients need), 8192x32768 505 and 466.
 constexpr int64_t kHeldCols = 16384;
 constexpr int kWideThreads = 256, kWideGroups = 64;
 
@@ -625,7 +627,11 @@ void set_rows(NormForm& f, int64_t M, int threads, int64_t units) {
 // and one from there on (bf16, two against one, us: 1280x12288 10.9 and 12.0, with a
 // checkpoint 16.5 and 18.7; 4096x12288 37.0 and 36.8, 44.9 and 45.0; 16384x12288 149 and
 // 144, 178 and 162; 16 waves and two chunks 13.1, 18.6, 40.4, 46.3, 145 and 168). Past that a row has 16 waves and they fit once
-// (eight waves of four chunks: 16384x13000 with a checkpoint 190, 16 waves 181).
+// (eight waves of four chunks: 16384x13000 with a checkpoint 190, 16 waves 181). Past 16384
+// columns, at four chunks a thread, 7 of the 128 registers go to scratch (24 bytes a
+// thread): bf16 8192x32768 209 us (5.1 TB/s), with a checkpoint 231 (5.9); 1024x32768 28.6
+// (4.7). Classes end at powers of two: a row just past one leaves half of the lanes
+// idle (33.5 million values: 4096 columns 24.9 us, 4160 30.9; 2048 25.8, 2112 34.0).
 NormForm norm_forward_form(int64_t M, int64_t N) {
     NormForm f{};
     f.threads = N <= 128 ? 8 : N <= 256 ? 16 : N <= 512 ? 32 : N <= 1024 ? 64 : N <= 2048 ? 128 : N <= 4096 ? 256 : N <= 12288 ? 512 : 1024;
@@ -637,7 +643,13 @@ NormForm norm_forward_form(int64_t M, int64_t N) {
 // Backward: one workgroup of 16 waves per compute unit. One chunk of a row per thread
 // while 16 waves take a row so: its registers leave room for the loads of three rows
 // ahead (16384x4096 bf16 from an int8 checkpoint 57 us, one row ahead 63, four 58; two
-// chunks and one row ahead 66, two rows ahead do not fit and take 140).
+// chunks and one row ahead 66, two rows ahead do not fit and take 140). 8193 to 12288 columns
+// have two chunks a thread and two rows ahead, 12289 to 16384 one row ahead on 16 waves, whose
+// 128 registers do not suffice: 3 go to scratch from x (16 bytes a thread), 9 from a
+// checkpoint (40 bytes). bf16, from x and from int8, the second launch not counted:
+// 8192x16384 154 us (5.2 TB/s) and 162 (4.2), 16384x13000 237 (5.4) and 256 (4.2), 4000x14336 63
+// (5.5) and 74 (3.9). Rows just past a class as in the forward pass: 4096 columns 34.2 us,
+// 4160 41.1; 2048 34.9, 2112 46.3.
 NormForm norm_backward_form(int64_t M, int64_t N) {
     NormForm f{};
     f.threads = N <= 64 ? 8 : N <= 128 ? 16 : N <= 256 ? 32 : N <= 512 ? 64 : N <= 1024 ? 128 : N <= 2048 ? 256

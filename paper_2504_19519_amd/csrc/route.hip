@@ -29,7 +29,11 @@ namespace fo {
 namespace {
 
 constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64;
-constexpr int64_t kSortAlone = 8192;        // pairs that one workgroup sorts by itself
+// Pairs that one workgroup sorts by itself: one launch and no workspace. The kernels'
+// time would draw the line lower (us, 8 / 64 / 256 experts: alone 1024 pairs 4.2 / 5.4 / 8.6,
+// 2048 5.6 / 7.2 / 10.7, 4096 8.4 / 10.6 / 14.9, 8192 14.1 / 17.9 / 23.1; 8200 in two launches
+// 9.1 / 10.0 / 11.8, 131072 10.3 / 11.2 / 13.7), a second launch aside.
+constexpr int64_t kSortAlone = 8192;
 constexpr int64_t kSortRun = 2048;          // pairs of one workgroup among several, at least
 constexpr int kSortBlocks = 256;            // workgroups, at most
 constexpr int kThreads = 256, kWaves = kThreads / 64;
