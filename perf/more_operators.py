@@ -22,7 +22,6 @@ import torch
 own = False
 
 EPS = 1e-6
-LEAST = 2.0 ** -126            # of a row's scale
 MOST_FLOPS, MOST_BYTES, MOST_WEIGHTS = 9.0e11, 1.2e9, 3.7e9      # of a drawn case
 _DTYPE = {"fp16": torch.float16, "bf16": torch.bfloat16}
 
@@ -235,8 +234,8 @@ def _plain(s):
     if op == "quantize":
         x = s["x"].float()
         top = x.abs().amax(dim=1, keepdim=True)
-        scales = (top / 127.0).clamp(min=LEAST)
-        codes = (x * 127.0 / top.clamp(min=127.0 * LEAST)).round()
+        scales = top / 127.0
+        codes = torch.where(top > 0, x * 127.0 / top, 0.0).round()
         return {"values": (codes * scales).to(dtype), "scales": scales.reshape(-1)}
     if op in ("norm_train", "norm_linear"):
         h = (s["x"].float() + s["residual"].float()).to(dtype)
@@ -249,8 +248,8 @@ def _plain(s):
             dx = s["dh"].float() + rstd * (g - hh * (g * hh).mean(dim=1, keepdim=True))
             return {"h": h, "y": y.to(dtype), "rstd": rstd.reshape(-1), "dx": dx.to(dtype), "dgamma": (dy * hh).sum(dim=0)}
         top = y.abs().amax(dim=1, keepdim=True)
-        a = (y * 127.0 / top.clamp(min=127.0 * LEAST)).round()
-        a_scales = (top / 127.0).clamp(min=LEAST)
+        a = torch.where(top > 0, y * 127.0 / top, 0.0).round()
+        a_scales = top / 127.0
     if op in ("norm_linear", "product"):
         H = case["H"]
         if op == "product":
@@ -298,8 +297,7 @@ def work(case):
 def _whole(v):
     """(codes, scales) of rows in 64 bits."""
     top = v.abs().max(dim=1, keepdim=True).values
-    scales = torch.maximum(top / 127, torch.full_like(top, LEAST))
-    return torch.round(v / scales), scales
+    return torch.round(127 * v / torch.where(top > 0, top, 1.0)), top / 127
 
 
 def exact(case, seed):
@@ -310,7 +308,7 @@ def exact(case, seed):
         return {"values": codes * scales, "scales": scales[:, 0]}
     if op in ("norm_train", "norm_linear"):
         h = s["x"].double() + s["residual"].double()
-        h16 = h.float().to(dtype).double()       # (a sum of two 16-bit values: 32 bits round it to a nearest 16-bit one's side)
+        h16 = h.float().to(dtype).double()       # (as it is kept)
         width = h.shape[1]
         rstd = (h16.square().sum(1) / width + EPS) ** -0.5
         if op == "norm_train":
