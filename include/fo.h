@@ -656,6 +656,100 @@ fo_status fo_route_combine_backward(int32_t dtype, int64_t T, int32_t K, int64_t
                                     void* drows, int64_t lddr, float* dweights, const int32_t* offsets,
                                     const int32_t* counts, int32_t E, void* stream);
 
+/* ---- 8-bit operators ----------------------------------------------------
+ *
+ * A linear layer or a mixture-of-experts block in 8-bit integers: rows put into 8
+ * bits with a scale each, the norm in front of such a layer with the residual's
+ * addition, and products of 8-bit matrices with scales for each token (row of a) and
+ * channel (row of b). They need no plan and keep to what stands above for the row
+ * operators: strides, sizes of zero, launches, overlap.
+ *
+ * A matrix of N columns in 8 bits is int8 codes in rows `ld` bytes apart (a multiple
+ * of 16, at least fo_int8_row_bytes(N), at most 2^22; 16-byte aligned), with an fp32
+ * scale for each row: value = code * scale. Codes behind a row's end, up to
+ * fo_int8_row_bytes(N) (N rounded up to a multiple of 16), are zeros.
+ */
+
+int64_t fo_int8_row_bytes(int64_t N);
+
+/*
+ * fo_quantize_rows -- per row of x [M, N] (any N up to 2^30): with m the row's largest
+ * magnitude, scale = m / 127 and code = 127 x / m, rounded to nearest even. A row of
+ * zeros has scale 0; a row with an infinity or a NaN has scale NaN and codes 0, and
+ * reads as NaN throughout. Weights (a row for each channel) are put into 8 bits by the
+ * same call. codes, scales and x must not overlap.
+ * Errors: FO_ERR_ARG, FO_ERR_SHAPE, FO_ERR_HIP.
+ */
+fo_status fo_quantize_rows(int32_t dtype, int64_t M, int64_t N, const void* x, int64_t ldx, void* codes, int64_t ldc,
+                           float* scales, void* stream);
+
+/*
+ * fo_norm_add_forward -- per row of x and residual [M, N], N <= 32768 (else
+ * FO_ERR_UNSUPPORTED):
+ *   h = x + residual, rounded to dtype (residual NULL: x), rstd = 1 / sqrt(sum(h^2) / N + eps),
+ *   y = h * rstd * gamma
+ * (RMS norm of h as it is kept). gamma: [N] of dtype, NULL = 1. Outputs, each of which
+ * may be NULL: h [M, N], the next residual; y [M, N] of dtype; codes and scales (both
+ * or neither), y in 8 bits by fo_quantize_rows' formula, y not rounded to dtype on the
+ * way; rstd [M] fp32, for the backward pass. y, or codes and scales, is asked for. h and
+ * y may each be x or residual (same ld), and must not overlap otherwise.
+ * Magnitudes of h up to 2^60 stay within fp32; products h * gamma are taken as fp32
+ * holds them (exact from 2^-126 to 2^128).
+ * Errors: FO_ERR_ARG, FO_ERR_UNSUPPORTED, FO_ERR_SHAPE, FO_ERR_HIP.
+ */
+fo_status fo_norm_add_forward(int32_t dtype, int64_t M, int64_t N, const void* x, int64_t ldx, const void* residual,
+                              int64_t ldr, const void* gamma, float eps, void* h, int64_t ldh, void* y, int64_t ldy,
+                              float* rstd, void* codes, int64_t ldc, float* scales, void* stream);
+
+/*
+ * fo_norm_add_backward -- the gradients of fo_norm_add_forward, h and rstd as it gave
+ * them, dy the gradient of y (of its 8-bit form too: rounding passes gradients on) and
+ * dh, or NULL, the one that reaches h from elsewhere. With g = dy * gamma:
+ *   dx = dh + rstd * (g - h * rstd^2 * sum(g * h) / N),   the gradient of x and of residual;
+ *   dgamma[n] = sum over rows of dy * h * rstd.
+ * dx [M, N] of dtype, dgamma [N] fp32: one of the two may be NULL. dx may be dy, dh or h
+ * (same ld). dgamma is overwritten (zeros for M = 0). It, and dx of rows of more than
+ * 16384 columns, need a workspace of fo_norm_workspace_bytes(M, N) bytes as
+ * fo_norm_backward has it.
+ */
+fo_status fo_norm_add_backward(int32_t dtype, int64_t M, int64_t N, const void* dy, int64_t lddy, const void* dh,
+                               int64_t lddh, const void* h, int64_t ldh, const void* gamma, const float* rstd, void* dx,
+                               int64_t lddx, float* dgamma, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * fo_int8_product -- c[m, n] = (sum over k of a[m, k] * b[n, k]) * a_scales[m] * b_scales[n]
+ * + bias[n]: c [M, N] of dtype, a [M, K] and b [N, K] in 8 bits (any codes, -128 too),
+ * bias [N] of dtype or NULL. The sum is exact (K <= 131071, else FO_ERR_UNSUPPORTED);
+ * it is rounded to fp32, multiplied in this order, and the result rounded to dtype. M, N
+ * and K are of any size (K = 0: the bias, or zeros). c must not overlap the others.
+ * workspace: fo_int8_workspace_bytes(M, N, K) bytes (0 for most sizes), 16-byte aligned,
+ * that no other call uses meanwhile (a graph keeps using it on replay).
+ * Errors: FO_ERR_ARG, FO_ERR_UNSUPPORTED, FO_ERR_SHAPE, FO_ERR_HIP.
+ */
+int64_t fo_int8_workspace_bytes(int64_t M, int64_t N, int64_t K);
+fo_status fo_int8_product(int32_t dtype, int64_t M, int64_t N, int64_t K, const void* a, int64_t lda, const float* a_scales,
+                          const void* b, int64_t ldb, const float* b_scales, const void* bias, void* c, int64_t ldc,
+                          void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * fo_int8_experts -- the experts' products of a mixture-of-experts block, over the rows
+ * that fo_route_sort has put in order (offsets [E + 1], counts [E]; no row is two
+ * experts'): for each row r in [offsets[e], offsets[e] + counts[e]) of expert e, below
+ * capacity,
+ *   c[r, n] = (sum over k of a[s, k] * b[e * N + n, k]) * a_scales[s] * b_scales[e * N + n]
+ *             + bias[e * N + n],
+ * s = pair_of[r] / choices (rows of tokens, taken as they stand: no fo_route_permute is
+ * needed), or r itself where pair_of is NULL. a [a_rows, K], b [E * N, K] in 8 bits, c
+ * [capacity, N] of dtype, pair_of [capacity], b_scales and bias (or NULL) [E * N]. All
+ * other rows of c -- padding, behind the last, with s outside [0, a_rows) -- are left
+ * as they were. Limits and rounding as in fo_int8_product; through pair_of, a spans at
+ * most 2^31 bytes (else FO_ERR_SHAPE).
+ */
+fo_status fo_int8_experts(int32_t dtype, int64_t capacity, int64_t N, int64_t K, int32_t E, const void* a, int64_t a_rows,
+                          int64_t lda, const float* a_scales, const int32_t* pair_of, int32_t choices, const void* b,
+                          int64_t ldb, const float* b_scales, const void* bias, const int32_t* offsets, const int32_t* counts,
+                          void* c, int64_t ldc, void* stream);
+
 /*
  * How the producer (GEMM epilogue) publishes a finished tile and how the
  * consumer reads a signalled group. All modes are correct; they differ in

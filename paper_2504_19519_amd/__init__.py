@@ -26,7 +26,8 @@ __all__ = [
     "FP16", "BF16", "TILE", "SUBTILE", "SUBTOKEN", "ROWMAJOR",
     "norm_forward", "norm_backward", "norm_workspace_bytes", "pack_rows", "unpack_rows", "packed_bytes",
     "route_sort", "route_permute", "route_combine", "route_combine_backward", "route_capacity",
-    "route_workspace_bytes", "LAYER_NORM", "RMS_NORM", "PACK_INT8", "PACK_E4M3",
+    "route_workspace_bytes", "quantize_rows", "norm_add_forward", "norm_add_backward", "int8_product", "int8_experts",
+    "int8_row_bytes", "int8_workspace_bytes", "LAYER_NORM", "RMS_NORM", "PACK_INT8", "PACK_E4M3",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libfo.so")
@@ -151,8 +152,17 @@ def lib() -> ctypes.CDLL:
     L.fo_route_combine.argtypes = [i32, i64, i32, i64, vp, i64, i64, vp, vp, vp, i64, vp, vp, i32, vp]
     L.fo_route_combine_backward.argtypes = [i32, i64, i32, i64, vp, i64, vp, i64, vp, vp, i32, i64, vp, vp, vp, i64,
                                             vp, vp, vp, i32, vp]
+    L.fo_int8_row_bytes.argtypes, L.fo_int8_row_bytes.restype = [i64], i64
+    L.fo_int8_workspace_bytes.argtypes, L.fo_int8_workspace_bytes.restype = [i64, i64, i64], i64
+    L.fo_quantize_rows.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, vp]
+    L.fo_norm_add_forward.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, f32, vp, i64, vp, i64, vp, vp, i64, vp, vp]
+    L.fo_norm_add_backward.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, i64, vp]
+    L.fo_int8_product.argtypes = [i32, i64, i64, i64, vp, i64, vp, vp, i64, vp, vp, vp, i64, vp, i64, vp]
+    L.fo_int8_experts.argtypes = [i32, i64, i64, i64, i32, vp, i64, i64, vp, vp, i32, vp, i64, vp, vp, vp, vp, vp, i64,
+                                  vp]
     for f in (L.fo_norm_forward, L.fo_norm_backward, L.fo_pack_rows, L.fo_unpack_rows, L.fo_route_sort,
-              L.fo_route_permute, L.fo_route_combine, L.fo_route_combine_backward):
+              L.fo_route_permute, L.fo_route_combine, L.fo_route_combine_backward, L.fo_quantize_rows,
+              L.fo_norm_add_forward, L.fo_norm_add_backward, L.fo_int8_product, L.fo_int8_experts):
         f.restype = ctypes.c_int
     L.fo_status_string.argtypes, L.fo_status_string.restype = [ctypes.c_int], ctypes.c_char_p
     L.fo_last_error.restype = ctypes.c_char_p
@@ -702,6 +712,48 @@ class _Args:
             raise ValueError(f"{what}: contiguous memory is needed")
         return x.data_ptr(), x.numel() * x.element_size()
 
+    def codes(self, x, M: int, N: int, ld, what: str):
+        """(pointer, row distance) of a [M, N] matrix in 8 bits, each of its rows a whole number
+        of 16 bytes: of shape [.., N] or, padded, [.., int8_row_bytes(N)] (dimensions ahead of
+        the last one together hold the rows), or one-dimensional storage."""
+        width = -(-N // 16) * 16
+        if x is None:
+            return None, width
+        try:
+            d = x.get_device()
+        except AttributeError:
+            return _ptr(x), width if ld is None else int(ld)
+        if d != self.device or d < 0:
+            self._place(d, what)
+        if x.dtype not in (_TYPES or _types())["u8"]:
+            raise ValueError(f"{what}: {x.dtype} values for 8-bit codes")
+        if ld is not None or x.dim() < 2 or M == 0 or N == 0:
+            ld = width if ld is None else int(ld)
+            if not x.is_contiguous() or x.numel() < ((M - 1) * ld + width if M > 0 and N > 0 else 0):
+                raise ValueError(f"{what}: contiguous codes are needed, {M} rows of {width} bytes, {ld} apart")
+            return x.data_ptr(), ld
+        shape = x.shape
+        length = shape[-1]
+        if length != N and length != width:
+            raise ValueError(f"{what}: shape {tuple(shape)} for rows of {N}: a [{M}, {N}] or [{M}, {width}] view or a row "
+                             f"distance is needed")
+        if x.dim() == 2:
+            have, (step, unit) = shape[0], x.stride()
+        elif x.is_contiguous():
+            have, step, unit = x.numel() // length, length, 1
+        else:
+            raise ValueError(f"{what}: more than two dimensions have to be contiguous")
+        if have < M:
+            raise ValueError(f"{what}: {have} rows, the call needs {M}")
+        if M == 1:
+            step = max(step, width)
+        if (unit != 1 and length > 1) or step < width:
+            raise ValueError(f"{what}: rows of unit stride, at least {width} bytes apart, are needed; strides are "
+                             f"{tuple(x.stride())}")
+        if length < width and x.storage_offset() + (M - 1) * step + width > x.untyped_storage().nbytes():
+            raise ValueError(f"{what}: the last row's codes end at {width} bytes, behind the tensor's memory")
+        return x.data_ptr(), step if M > 1 else width
+
     def pack(self, packed, scales, M: int, N: int, fmt):
         """(packed, scales, format) of an [M, N] checkpoint."""
         if packed is None and scales is None:
@@ -839,3 +891,87 @@ def route_combine_backward(dout, rows, slot_of, weights, drows, dweights, T: int
                                            a.flat(dweights, T * K, "dweights", "f32", K),
                                            a.flat(offsets, E + 1, "offsets", "i32"),
                                            a.flat(counts, E, "counts", "i32"), E, _stream(stream)))
+
+
+# ---- 8-bit operators ----------------------------------------------------------
+
+def int8_row_bytes(N: int) -> int:
+    """fo_int8_row_bytes: bytes of a row of N codes (a multiple of 16)."""
+    return lib().fo_int8_row_bytes(N)
+
+
+def int8_workspace_bytes(M: int, N: int, K: int) -> int:
+    """fo_int8_workspace_bytes: what int8_product needs (0: nothing)."""
+    return lib().fo_int8_workspace_bytes(M, N, K)
+
+
+def quantize_rows(x, codes, scales, M: int, N: int, dtype, ldx=None, ldc=None, stream=None) -> None:
+    """fo_quantize_rows: x [M, N] as int8 codes ([M, int8_row_bytes(N)]) and a scale
+    ([M] fp32) per row, value = code * scale."""
+    a = _Args(dtype, stream)
+    px, sx = a.rows(x, M, N, ldx, "x")
+    pc, sc = a.codes(codes, M, N, ldc, "codes")
+    _check(lib().fo_quantize_rows(a.dtype, M, N, px, sx, pc, sc, a.flat(scales, M, "scales", "f32"), _stream(stream)))
+
+
+def norm_add_forward(x, residual, gamma, h, y, M: int, N: int, dtype, eps: float = 1e-6, rstd=None, codes=None,
+                     scales=None, ldx=None, ldr=None, ldh=None, ldy=None, ldc=None, stream=None) -> None:
+    """fo_norm_add_forward: h = x + residual, y = RMS norm of h, in 16 bits (y), as codes
+    and scales, or both. residual, gamma, h, y and rstd ([M] fp32) may be None."""
+    a = _Args(dtype, stream)
+    px, sx = a.rows(x, M, N, ldx, "x")
+    pr, sr = a.rows(residual, M, N, ldr, "residual")
+    ph, sh = a.rows(h, M, N, ldh, "h")
+    py, sy = a.rows(y, M, N, ldy, "y")
+    pc, sc = a.codes(codes, M, N, ldc, "codes")
+    _check(lib().fo_norm_add_forward(a.dtype, M, N, px, sx, pr, sr, a.flat(gamma, N, "gamma"), eps, ph, sh, py, sy,
+                                     a.flat(rstd, M, "rstd", "f32"), pc, sc, a.flat(scales, M, "scales", "f32"),
+                                     _stream(stream)))
+
+
+def norm_add_backward(dy, dh, h, gamma, rstd, dx, dgamma, M: int, N: int, dtype, workspace=None, lddy=None, lddh=None,
+                      ldh=None, lddx=None, stream=None) -> None:
+    """fo_norm_add_backward: dx, the gradient of x and residual, and dgamma (fp32; either
+    may be None) from dy, the gradient of y, and dh (or None), h's from elsewhere. workspace:
+    norm_workspace_bytes(M, N)."""
+    a = _Args(dtype, stream)
+    pg, sg = a.rows(dy, M, N, lddy, "dy")
+    pd, sd = a.rows(dh, M, N, lddh, "dh")
+    ph, sh = a.rows(h, M, N, ldh, "h")
+    px, sx = a.rows(dx, M, N, lddx, "dx")
+    work, size = a.space(workspace)
+    _check(lib().fo_norm_add_backward(a.dtype, M, N, pg, sg, pd, sd, ph, sh, a.flat(gamma, N, "gamma"),
+                                      a.flat(rstd, M, "rstd", "f32"), px, sx, a.flat(dgamma, N, "dgamma", "f32"), work,
+                                      size, _stream(stream)))
+
+
+def int8_product(a, a_scales, b, b_scales, c, M: int, N: int, K: int, dtype, bias=None, workspace=None, lda=None,
+                 ldb=None, ldc=None, stream=None) -> None:
+    """fo_int8_product: c [M, N] = a [M, K] times b [N, K] transposed, both int8 codes,
+    with a_scales [M] and b_scales [N] (fp32) and bias [N]. workspace:
+    int8_workspace_bytes(M, N, K)."""
+    args = _Args(dtype, stream)
+    pa, sa = args.codes(a, M, K, lda, "a")
+    pb, sb = args.codes(b, N, K, ldb, "b")
+    pc, sc = args.rows(c, M, N, ldc, "c")
+    work, size = args.space(workspace)
+    _check(lib().fo_int8_product(args.dtype, M, N, K, pa, sa, args.flat(a_scales, M, "a_scales", "f32"), pb, sb,
+                                 args.flat(b_scales, N, "b_scales", "f32"), args.flat(bias, N, "bias"), pc, sc, work,
+                                 size, _stream(stream)))
+
+
+def int8_experts(a, a_scales, b, b_scales, c, N: int, K: int, E: int, dtype, capacity: int, offsets, counts, rows: int,
+                 pair_of=None, choices: int = 1, bias=None, lda=None, ldb=None, ldc=None, stream=None) -> None:
+    """fo_int8_experts: each row of c [capacity, N] in expert e's range of route_sort's
+    offsets and counts = its row of a [rows, K] times b[e] ([E, N, K]) transposed, with the
+    scales and bias ([E, N]) of that expert. Its row of a: pair_of's token (choices per
+    token), or without pair_of the row of the same number."""
+    args = _Args(dtype, stream)
+    pa, sa = args.codes(a, rows, K, lda, "a")
+    pb, sb = args.codes(b, E * N, K, ldb, "b")
+    pc, sc = args.rows(c, capacity, N, ldc, "c")
+    _check(lib().fo_int8_experts(args.dtype, capacity, N, K, E, pa, rows, sa, args.flat(a_scales, rows, "a_scales", "f32"),
+                                 args.flat(pair_of, capacity, "pair_of", "i32"), choices, pb, sb,
+                                 args.flat(b_scales, E * N, "b_scales", "f32", N), args.flat(bias, E * N, "bias", None, N),
+                                 args.flat(offsets, E + 1, "offsets", "i32"), args.flat(counts, E, "counts", "i32"), pc, sc,
+                                 _stream(stream)))

@@ -702,13 +702,14 @@ hipError_t launch_norm_backward(int dtype, const NormArgs& a, float* dgamma, flo
             return dtype == FO_FP16 ? from(Int<FO_FP16>()) : from(Int<FO_BF16>());
         });
     }
-    if (e == hipSuccess && (dgamma || dbeta)) {
-        const int count = a.M > 0 ? (int)f.blocks : 0;
-        const int64_t per = (norm_partial_cols(a.N) + kReduceCols - 1) / kReduceCols;
-        e = launch(norm_reduce_kernel, (uint32_t)(per * (dgamma && dbeta ? 2 : 1)), kReduceThreads, s, a.partial, count, a.N,
-                   dgamma, dbeta);
-    }
-    return e;
+    return e == hipSuccess && (dgamma || dbeta)
+               ? launch_norm_reduce(a.partial, a.M > 0 ? (int)f.blocks : 0, a.N, dgamma, dbeta, s) : e;
+}
+
+hipError_t launch_norm_reduce(const float* partial, int count, int64_t N, float* dgamma, float* dbeta, hipStream_t s) {
+    const int64_t per = (norm_partial_cols(N) + kReduceCols - 1) / kReduceCols;
+    return launch(norm_reduce_kernel, (uint32_t)(per * (dgamma && dbeta ? 2 : 1)), kReduceThreads, s, partial, count, N, dgamma,
+                  dbeta);
 }
 
 }  // namespace fo

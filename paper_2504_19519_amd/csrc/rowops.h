@@ -60,6 +60,8 @@ int64_t norm_dots_bytes(int64_t M, int64_t N);
 hipError_t launch_norm_forward(int dtype, const NormArgs& a, hipStream_t s);
 // The sums over rows go to a.partial; then dgamma and dbeta (each or null) are their sums.
 hipError_t launch_norm_backward(int dtype, const NormArgs& a, float* dgamma, float* dbeta, hipStream_t s);
+// dgamma and dbeta (one may be null): the sums of `count` rows of partial sums.
+hipError_t launch_norm_reduce(const float* partial, int count, int64_t N, float* dgamma, float* dbeta, hipStream_t s);
 
 struct PackArgs {
     uint16_t* x;                // [M] rows, ldx apart
