@@ -39,11 +39,12 @@ def product(a, a_scales, b, b_scales, bias=None):
 
 def experts(a, a_scales, b, b_scales, offsets, counts, capacity, pair_of=None, choices=1, bias=None):
     """{row: (values, magnitude)} of the rows that are written: b [E, N, K]."""
-    out = {}
+    out, pair_of = {}, None if pair_of is None else np.asarray(pair_of)
     for e in range(len(counts)):
-        for r in range(int(offsets[e]), min(int(offsets[e]) + int(counts[e]), capacity)):
-            s = r if pair_of is None else int(pair_of[r]) // choices if pair_of[r] >= 0 else -1
-            if 0 <= s < len(a):
-                c, mag = product(a[s:s + 1], a_scales[s:s + 1], b[e], b_scales[e], None if bias is None else bias[e])
-                out[r] = (c[0], mag[0])
+        rows = np.arange(int(offsets[e]), min(int(offsets[e]) + int(counts[e]), capacity))
+        src = rows if pair_of is None else np.where(pair_of[rows] >= 0, pair_of[rows] // choices, -1)
+        rows, src = rows[(src >= 0) & (src < len(a))], src[(src >= 0) & (src < len(a))]
+        if len(rows):
+            c, mag = product(a[src], a_scales[src], b[e], b_scales[e], None if bias is None else bias[e])
+            out.update((int(r), (c[i], mag[i])) for i, r in enumerate(rows))
     return out

@@ -20,7 +20,7 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libfo.so")
 USAGE = os.path.join(OBJ, "resource_usage.json")
 SOURCES = ["plan.cpp", "gemm.hip", "gemm_block.hip", "consume.hip", "post.hip", "norm.hip", "pack.hip", "route.hip",
-           "rowops.hip", "rows8.hip", "int8.hip", "int8ops.hip", "runtime.hip"]
+           "rowops.hip", "rows8.hip", "int8.hip", "int8_tile.hip", "int8ops.hip", "runtime.hip"]
 ARCH = "gfx950"
 
 

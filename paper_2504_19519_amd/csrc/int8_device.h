@@ -1,0 +1,176 @@
+// Device helpers of the 8-bit products: which block of the result a workgroup computes,
+// its rows of a, and a finished sum.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+#include <utility>
+
+#include "fo_device.h"
+#include "fo_internal.h"
+#include "int8ops.h"
+
+namespace fo {
+
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void lds_void_t;
+
+constexpr int wait_imm(int vm, int lgkm) {
+    return (vm & 15) | (7 << 4) | ((lgkm & 15) << 8) | (((vm >> 4) & 3) << 14);
+}
+constexpr int kRsrcWord3 = 0x00020000;          // raw byte-addressed buffer accesses
+constexpr uint32_t kSpan = 0x80000000u;         // bytes that a buffer resource covers
+constexpr uint32_t kOutside = kSpan;            // an offset past it: reads zeros, no memory access
+
+template <typename F, int... Is>
+__device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, Is...>) {
+    (f(std::integral_constant<int, Is>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+    static_for_impl(f, std::make_integer_sequence<int, N>{});
+}
+
+__device__ __forceinline__ i32x4_t mfma16(u32x4_t x, u32x4_t y, i32x4_t c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(bit_cast<i32x4_t>(x), bit_cast<i32x4_t>(y), c, 0, 0, 0);
+}
+
+// This wave waits until at most VM of its vector memory operations are in flight and all
+// of its LDS reads have returned, then meets the others.
+template <int VM>
+__device__ __forceinline__ void wait_and_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(wait_imm(VM, 0));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Where a workgroup's block of the result lies.
+struct Block {
+    int64_t row0, col0;         // of c
+    int rows;                   // that it has
+    int expert;
+};
+
+// Sums over lanes 0 .. l, in lane l.
+__device__ __forceinline__ int lanes_before(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, true);
+    return v;
+}
+
+// The block of workgroup `p` of those of BM rows and `width` columns; false: none. Experts:
+// every wave adds up the experts' blocks.
+template <int BM, bool EXPERTS>
+__device__ __forceinline__ bool find_block(const Int8Args& a, int p, int width, Block& b) {
+    const int cols = (int)((a.N + width - 1) / width);
+    constexpr int kXcds = 8;
+    if constexpr (!EXPERTS) {
+        const int rows = (int)((a.M + BM - 1) / BM), blocks = rows * cols;
+        const int t = tile_of_position(p, rows, cols, FO_ORDER_XCD, rows < 4 ? rows : 4, blocks < kXcds ? blocks : kXcds);
+        b.row0 = (int64_t)(t / cols) * BM;
+        b.col0 = (int64_t)(t % cols) * width;
+        b.rows = (int)(a.M - b.row0 < BM ? a.M - b.row0 : BM);
+        b.expert = 0;
+        return true;
+    } else {
+        // lane l adds up the row blocks of experts l run .. l run + run - 1
+        const int lane = threadIdx.x & 63, run = (a.E + 63) / 64;
+        // an expert's rows below the capacity
+        const auto rows_of = [&](int n, int o) {
+            const int most = o < 0 || o > a.capacity ? 0 : a.capacity - o;
+            return n < 0 ? 0 : n > most ? most : n;
+        };
+        int mine = 0;
+#pragma unroll 4
+        for (int i = 0; i < run; ++i) {
+            const int e = lane * run + i;
+            if (e < a.E) mine += (rows_of(a.counts[e], a.offsets[e]) + BM - 1) / BM;
+        }
+        const int upto = lanes_before(mine), total = __builtin_amdgcn_readlane(upto, 63);
+        // each chiplet takes a contiguous share of the blocks, an expert's after another's
+        const int64_t all = (int64_t)total * cols, per = (all + kXcds - 1) / kXcds;
+        const int64_t l = p / kXcds, t = (int64_t)(p % kXcds) * per + l;
+        if (l >= per || t >= all) return false;
+        const int at = (int)(t / cols);             // among the experts' row blocks
+        const int owner = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > at));
+        const int before = __builtin_amdgcn_readlane(upto, owner) - __builtin_amdgcn_readlane(mine, owner);
+        // the owner's experts, one to a lane
+        const int e = owner * run + lane;
+        const bool there = lane < run && e < a.E;
+        const int o_mine = there ? a.offsets[e] : 0, n_mine = there ? rows_of(a.counts[e], o_mine) : 0;
+        const int past = before + lanes_before((n_mine + BM - 1) / BM);
+        const int w = __builtin_ctzll(__builtin_amdgcn_ballot_w64(past > at));
+        const int expert = owner * run + w, n = __builtin_amdgcn_readlane(n_mine, w), o = __builtin_amdgcn_readlane(o_mine, w);
+        const int first = __builtin_amdgcn_readlane(past, w) - (n + BM - 1) / BM;
+        // (an expert's row blocks side by side: they share its weights)
+        const int inside = (int)(t - (int64_t)first * cols), high = (n + BM - 1) / BM, r = inside % high * BM;
+        b.expert = expert;
+        b.row0 = (int64_t)o + r;
+        b.col0 = (int64_t)(inside / high) * width;
+        b.rows = n - r < BM ? n - r : BM;
+        return true;
+    }
+}
+
+// The row of a that row r of the block is of; -1: none.
+template <bool EXPERTS>
+__device__ __forceinline__ int64_t source_row(const Int8Args& a, const Block& b, int r) {
+    if (r >= b.rows) return -1;
+    if constexpr (EXPERTS) {
+        int64_t s = b.row0 + r;
+        if (a.pair_of) {
+            const int pair = a.pair_of[s];
+            s = pair < 0 ? -1 : pair / a.choices;
+        }
+        return s < a.a_rows ? s : -1;
+    } else {
+        return b.row0 + r;
+    }
+}
+
+// A row's four results of the columns n .. n + 3.
+struct Columns {
+    float scale[4], bias[4];
+};
+template <int DT>
+__device__ __forceinline__ Columns columns_of(const Int8Args& a, int64_t expert, int64_t n) {
+    Columns c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const bool there = n + e < a.N;
+        const int64_t at = expert * a.N + n + e;
+        c.scale[e] = there ? a.b_scales[at] : 0.0f;
+        c.bias[e] = there && a.bias ? to_f32<DT>(a.bias[at]) : 0.0f;
+    }
+    return c;
+}
+template <int DT>
+__device__ __forceinline__ u32x2_t finish(i32x4_t sum, float scale, const Columns& c) {
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (float)sum[e] * scale * c.scale[e] + c.bias[e];
+    return u32x2_t{pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
+}
+
+// The `left` first of four results, at any 2-byte aligned address.
+__device__ __forceinline__ void write_four(uint16_t* p, u32x2_t v, int64_t left) {
+    if (left >= 4) {
+        __builtin_memcpy(p, &v, sizeof(v));
+    } else if (left > 0) {
+        p[0] = (uint16_t)v[0];
+        if (left > 1) p[1] = (uint16_t)(v[0] >> 16);
+        if (left > 2) p[2] = (uint16_t)v[1];
+    }
+}
+
+// Columns of the sums of a part of k: whole groups of four, so that every row is 16-byte aligned.
+FO_HD inline int64_t partial_cols(int64_t N) { return (N + 3) / 4 * 4; }
+
+}  // namespace fo

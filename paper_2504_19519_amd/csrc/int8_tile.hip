@@ -1,0 +1,207 @@
+// Products of 8-bit matrices in tiles of 256 x 256 (gfx950).
+//
+// Four waves, one per SIMD, each on 128 x 128 of the tile: an operand byte that is read
+// from LDS feeds 64 products, twice as many as in a 128 x 128 tile's waves of 64 x 64, whose
+// LDS reads bound them. k steps of 128 move from memory straight into an LDS ring of two
+// stages; v_mfma_i32_16x16x64_i8 in inline asm with the accumulators tied in place, every
+// LDS read and load issue in the shadow of an MFMA. The scales, the bias and the rows' places
+// wait in LDS from the tile's start.
+#include <hip/hip_runtime.h>
+
+#include "int8_device.h"
+#include "rows.h"
+#include "rowops.h"
+
+namespace fo {
+namespace {
+
+// The accumulator is tied in place (dst = srcC), in VGPRs with KEEP_V and in AGPRs without:
+// with 256 accumulator registers the compiler's own MFMAs get copied between the register
+// files. The compiler does not track the hazards of these instructions: accumulators are
+// never written by VALU right before one (the first MFMA of a tile takes srcC = 0) and read
+// only after the wait that ends the main loop.
+template <bool FIRST, bool KEEP_V>
+__device__ __forceinline__ void mfma_tied(i32x4_t& c, const u32x4_t& x, const u32x4_t& y) {
+    if constexpr (FIRST && KEEP_V) asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, 0" : "=v"(c) : "v"(x), "v"(y));
+    else if constexpr (FIRST) asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, 0" : "=a"(c) : "v"(x), "v"(y));
+    else if constexpr (KEEP_V) asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+v"(c) : "v"(x), "v"(y));
+    else asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(x), "v"(y));
+}
+
+template <int DT, bool EXPERTS>
+__global__ __launch_bounds__(256, 1) void int8_tile_kernel(const Int8Args a) {
+    constexpr int BM = 256, BN = 256, WT = 128, MI = 8, NJ = 8;
+    constexpr int kA = BM * 128, kStage = (BM + BN) * 128;
+    constexpr int kHalf = 8, kLoads = 16;                // load instructions of A, and of both, per wave and step
+    constexpr int kVRows = 2;                            // accumulator block rows held in VGPRs
+
+    // the stages live in separate arrays, so that the compiler can tell the stage being
+    // read from the stage being filled
+    __shared__ __attribute__((aligned(1024))) char st0[kStage];
+    __shared__ __attribute__((aligned(1024))) char st1[kStage];
+    __shared__ __attribute__((aligned(16))) float s_scale[BN], s_bias[BN], s_row[BM];
+    __shared__ bool s_there[BM];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+    Block b;
+    if (!find_block<BM, EXPERTS>(a, blockIdx.x, BN, b)) return;
+    const uint32_t bytes = (uint32_t)int8_row_bytes(a.K);
+    const int steps = (int)((bytes + 127) / 128);
+    const bool gather = EXPERTS && a.pair_of;
+    const int8_t* const ablk = gather ? a.a : a.a + b.row0 * a.lda;
+    const int8_t* const bblk = a.b + ((int64_t)b.expert * a.N + b.col0) * a.ldb;
+    const int cols = (int)(a.N - b.col0 < BN ? a.N - b.col0 : BN);
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)ablk, 0, (int)kSpan, kRsrcWord3);
+    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc((void*)bblk, 0, (int)kSpan, kRsrcWord3);
+
+    // A load instruction fills 1 KB: 8 operand rows of 128 bytes, chunk c of row r at slot
+    // c ^ ((r / 2) % 8). A lane's offset from the operand's base, or kOutside for a row that
+    // is not there; its place in the row goes by whether the instruction's number is odd.
+    uint32_t voff[kLoads], place[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) place[i] = 16u * (uint32_t)((lane & 7) ^ ((4 * i + lane / 16) & 7));
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int r = (wave * kHalf + i % kHalf) * 8 + lane / 8;
+        if (i < kHalf) {
+            const int64_t s = source_row<EXPERTS>(a, b, r);
+            voff[i] = s < 0 ? kOutside : (uint32_t)((gather ? s : r) * a.lda) + place[i & 1];
+        } else {
+            voff[i] = r < cols ? (uint32_t)(r * a.ldb) + place[i & 1] : kOutside;
+        }
+    }
+    // Load `i` of step t. Chunks past a row's end, and steps past the last, lie outside the
+    // resource: zeros, no memory access (every step issues the same loads, and the wait
+    // counts stay uniform). The step's offset past kOutside stays outside.
+    auto load_one = [&](auto ic, int t, char* st) __attribute__((always_inline)) {
+        constexpr int i = decltype(ic)::value;
+        const uint32_t at = 128u * (uint32_t)t;
+        const uint32_t v = place[i & 1] + at < bytes ? voff[i] : kOutside;
+        if constexpr (i < kHalf)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void_t*)(st + (wave * kHalf + i) * 1024), 16, v, at, 0, 0);
+        else
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void_t*)(st + kA + (wave * kHalf + i - kHalf) * 1024), 16, v, at, 0, 0);
+    };
+
+    // Fragments: lane l feeds row l % 16 of a 16-row block with chunk 4 h + l / 16 of MFMA
+    // substep h. The weights are the first operand: each lane holds four consecutive columns
+    // of a row of c.
+    const int a_row = (wm * WT + (lane & 15)) * 128, b_row = kA + (wn * WT + (lane & 15)) * 128;
+    int cslot[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) cslot[h] = 16 * ((4 * h + (lane >> 4)) ^ ((lane >> 1) & 7));
+    i32x4_t acc[MI][NJ];
+    u32x4_t fa0[MI], fb0[NJ], fa1[MI], fb1[NJ];
+    // MFMA m of a substep carries fragment read m of the next one (the order in which that
+    // needs them) and, with `loads`, every fourth one a load of the stage just freed.
+    auto substep = [&](const u32x4_t (&xa)[MI], const u32x4_t (&xb)[NJ], const char* rst, auto h_next, u32x4_t (&ya)[MI],
+                       u32x4_t (&yb)[NJ], auto loads, int t, char* lst, auto first) __attribute__((always_inline)) {
+        constexpr int h = decltype(h_next)::value;
+        static_for<MI * NJ>([&](auto mc) __attribute__((always_inline)) {
+            constexpr int m = decltype(mc)::value, i = m / NJ, j = m % NJ;
+            if constexpr (m == 0) ya[0] = *reinterpret_cast<const u32x4_t*>(rst + a_row + cslot[h]);
+            else if constexpr (m <= NJ) yb[m - 1] = *reinterpret_cast<const u32x4_t*>(rst + b_row + (m - 1) * 2048 + cslot[h]);
+            else if constexpr (m < MI + NJ) ya[m - NJ] = *reinterpret_cast<const u32x4_t*>(rst + a_row + (m - NJ) * 2048 + cslot[h]);
+            if constexpr (decltype(loads)::value && m % 4 == 0) load_one(std::integral_constant<int, m / 4>{}, t, lst);
+            mfma_tied<decltype(first)::value, (i >= MI - kVRows)>(acc[i][j], xb[j], xa[i]);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    // Step t (its first fragments are there) in stage cur, step t + 1 in nxt: once that has
+    // landed and every wave has read all of cur, step t + 2 goes there.
+    constexpr std::true_type kYes{};
+    constexpr std::false_type kNo{};
+    constexpr std::integral_constant<int, 0> k0{};
+    constexpr std::integral_constant<int, 1> k1{};
+    // What the epilogue wants to know of column `tid` and row `tid`, looked up behind the
+    // first loads and put into LDS at the first barrier.
+    float col_scale = 0.0f, col_bias = 0.0f, row_scale = 0.0f;
+    bool there = false;
+    auto step = [&](int t, char* cur, const char* nxt, auto first) __attribute__((always_inline)) {
+        substep(fa0, fb0, cur, k1, fa1, fb1, kNo, 0, cur, first);
+        wait_and_barrier<0>();
+        if constexpr (decltype(first)::value) {
+            s_scale[tid] = col_scale;
+            s_bias[tid] = col_bias;
+            s_row[tid] = row_scale;
+            s_there[tid] = there;
+        }
+        substep(fa1, fb1, nxt, k0, fa0, fb0, kYes, t + 2, cur, kNo);
+    };
+
+    static_for<kLoads>([&](auto ic) __attribute__((always_inline)) { load_one(ic, 0, st0); });
+    static_for<kLoads>([&](auto ic) __attribute__((always_inline)) { load_one(ic, 1, st1); });
+    {
+        const int64_t s = source_row<EXPERTS>(a, b, tid);
+        there = s >= 0;
+        if (there) row_scale = a.a_scales[s];
+        if (tid < cols) {
+            const int64_t at = (int64_t)b.expert * a.N + b.col0 + tid;
+            col_scale = a.b_scales[at];
+            if (a.bias) col_bias = to_f32<DT>(a.bias[at]);
+        }
+    }
+    wait_and_barrier<0>();
+    fa0[0] = *reinterpret_cast<const u32x4_t*>(st0 + a_row + cslot[0]);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) fb0[j] = *reinterpret_cast<const u32x4_t*>(st0 + b_row + j * 2048 + cslot[0]);
+#pragma unroll
+    for (int i = 1; i < MI; ++i) fa0[i] = *reinterpret_cast<const u32x4_t*>(st0 + a_row + i * 2048 + cslot[0]);
+    step(0, st0, st1, kYes);
+    int t = 1;
+    for (; t + 2 <= steps; t += 2) {
+        step(t, st1, st0, kNo);
+        step(t + 1, st0, st1, kNo);
+    }
+    if (t < steps) step(t, st1, st0, kNo);
+    // the accumulators are read only once the last MFMA's result is written
+    asm volatile("s_nop 7\n s_nop 7\n s_nop 7\n s_nop 7" ::: "memory");
+    wait_and_barrier<0>();          // no load may still be writing LDS
+    __syncthreads();                // the stages are reused for the result
+
+    // Row r of the tile is staged in 512 bytes: row r % 128 of stage r / 128 (the half of the
+    // waves' rows), chunk c at c ^ (r % 32), so that the rows that are written or read
+    // together lie on different banks.
+    int tid_e = tid;
+    asm volatile("" : "+v"(tid_e)); // the epilogue's addresses are formed here, not ahead of the main loop
+    const int lane_e = tid_e & 63, lr = lane_e & 15, lh = (lane_e >> 4) & 1, lq = lane_e >> 5;
+    char* const sb = wm == 0 ? st0 : st1;
+    static_for<NJ>([&](auto jc) __attribute__((always_inline)) {
+        constexpr int j = decltype(jc)::value;
+        const int col = wn * WT + j * 16 + 4 * (lane_e >> 4);
+        const f32x4_t scale = *reinterpret_cast<const f32x4_t*>(s_scale + col);
+        const f32x4_t bias = *reinterpret_cast<const f32x4_t*>(s_bias + col);
+        static_for<MI>([&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value;
+            const float row = s_row[wm * WT + i * 16 + lr];
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = (float)acc[i][j][e] * row * scale[e] + bias[e];
+            const u32x2_t w = {pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
+            const int r = i * 16 + lr, c = wn * 16 + 2 * j + lq;
+            *reinterpret_cast<u32x2_t*>(sb + r * 512 + ((c ^ (r & 31)) << 4) + 8 * lh) = w;
+        });
+    });
+    __syncthreads();
+    const int c = tid_e & 31, r0 = tid_e >> 5;
+    const int64_t left = cols - 8 * c;
+    uint16_t* const out = a.c + b.row0 * a.ldc + b.col0 + 8 * c;
+#pragma unroll 8
+    for (int k = 0; k < 32; ++k) {
+        const int r = r0 + 8 * k;
+        const char* const from = (k < 16 ? st0 : st1) + (r & 127) * 512 + ((c ^ (r & 31)) << 4);
+        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(from);
+        if (s_there[r]) write_chunk(out + (int64_t)r * a.ldc, v, left);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_int8_tile(int dtype, bool experts, uint32_t blocks, const Int8Args& a, hipStream_t s) {
+    if (experts)
+        return launch(dtype == FO_FP16 ? int8_tile_kernel<FO_FP16, true> : int8_tile_kernel<FO_BF16, true>, blocks, 256, s, a);
+    return launch(dtype == FO_FP16 ? int8_tile_kernel<FO_FP16, false> : int8_tile_kernel<FO_BF16, false>, blocks, 256, s, a);
+}
+
+}  // namespace fo

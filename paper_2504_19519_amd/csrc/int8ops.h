@@ -52,7 +52,7 @@ struct Int8Args {
     const float* b_scales;      // [N]; [E * N]
     const uint16_t* bias;       // [N]; [E * N]; or null
     uint16_t* c;                // rows, ldc apart
-    int32_t* partial;           // sums of parts of K, where it is split
+    int32_t* partial;           // [parts][M][partial_cols(N)] sums over a part of K each, where it is split
     int64_t M, N, K, lda, ldb, ldc;
     // by experts: expert e's rows of c are offsets[e] .. offsets[e] + counts[e] - 1
     const int32_t* offsets;
@@ -60,10 +60,14 @@ struct Int8Args {
     const int32_t* pair_of;     // row r is of a's row pair_of[r] / choices; null: a's row r
     int64_t a_rows;
     int32_t E, choices, capacity;
+    int32_t parts;              // of K; 1: not split
+    int32_t span;               // blocks, side by side, of a workgroup
 };
 int64_t int8_workspace_bytes(int64_t M, int64_t N, int64_t K);
 // Whether a launch takes the product (work-items are counted in 32 bits).
 bool int8_launchable(const Int8Args& a, bool experts);
+// Tiles of 256 x 256 (K > 0); `blocks` workgroups, a tile each.
+hipError_t launch_int8_tile(int dtype, bool experts, uint32_t blocks, const Int8Args& a, hipStream_t s);
 hipError_t launch_int8_product(int dtype, const Int8Args& a, hipStream_t s);
 hipError_t launch_int8_experts(int dtype, const Int8Args& a, hipStream_t s);
 

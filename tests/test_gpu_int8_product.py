@@ -82,6 +82,21 @@ def test_products(dtype, M, N, K):
     check(M, N, K, dtype)
 
 
+@pytest.mark.parametrize("M,N,K,bias", [(4096, 4096, 512, False), (4000, 4090, 700, True), (16384, 1030, 400, False),
+                                        (3900, 8200, 127, True), (8200, 4097, 40, False), (12000, 1500, 1300, True)])
+def test_large_tiles(M, N, K, bias):
+    """Enough 256 x 256 tiles for every compute unit, whole and ragged."""
+    check(M, N, K, "bf16", bias=bias, ldc=N + 1, shift=1)
+
+
+@pytest.mark.parametrize("M,N,K", [(16, 256, 16384), (1, 1, 8192), (5, 130, 8200), (40, 300, 9001), (64, 1027, 12288),
+                                   (128, 1000, 8177), (33, 18, 131071)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_inner_sizes_that_are_split(M, N, K, bias):
+    assert fo.int8_workspace_bytes(M, N, K) > 0
+    check(M, N, K, "fp16", bias=bias, ldc=N + 5)
+
+
 @pytest.mark.parametrize("M", [3, 20, 50, 90, 400])
 def test_rows_apart(M):
     """Strides of all three matrices, guards between their rows (the codes' are no zeros)."""
@@ -185,6 +200,19 @@ def test_one_busy_expert(T):
     Experts(T, 1, 64, 40, 80, "bf16", True, busy=[63]).check()
     Experts(T, 1, 130, 40, 80, "bf16", False, busy=[0], align=64).check()
     Experts(T, 2, 100, 40, 80, "bf16", True, busy=[17, 70]).check()
+
+
+@pytest.mark.parametrize("T,K,E,N,H,gather", [(4096, 2, 4, 2048, 512, True), (3000, 2, 3, 2990, 600, False), (2500, 2, 8, 3001, 300, True),
+                                              (6000, 4, 30, 700, 200, True)])
+def test_experts_large_tiles(T, K, E, N, H, gather):
+    Experts(T, K, E, N, H, "bf16", gather, align=64, drop=0.05, bias=True).check()
+
+
+@pytest.mark.parametrize("H", [16, 100, 500, 1500])
+def test_experts_several_blocks_to_a_workgroup(H):
+    """Short sums and many columns."""
+    Experts(40, 4, 60, 2300, H, "fp16", True, bias=True).check()
+    Experts(1000, 2, 16, 2300, min(H, 500), "bf16", False).check()
 
 
 def test_experts_rows_apart():

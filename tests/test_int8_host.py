@@ -82,6 +82,11 @@ def test_product_refusals():
     refused(SHAPE, call, M=1 << 24, N=1 << 24, c=1 << 60, b=1 << 55)
     call(M=0, a=None, a_scales=None, c=None)
     call(N=0, b=None, b_scales=None, c=None)
+    need = fo.int8_workspace_bytes(4, 8, 16384)
+    assert need >= 2 * 4 * 8 * 4
+    args = [0, 4, 8, 16384, P, 16384, 2 * P, 3 * P, 16384, 4 * P, None, 5 * P, 8]
+    for bad in ([None, 1 << 40, None], [9 * P, need - 1, None], [9 * P + 8, need, None]):
+        assert fo.lib().fo_int8_product(*args, *bad) == ARG and b"workspace" in fo.lib().fo_last_error()
     for bad in (-1, 0, 1 << 40):
         assert fo.int8_workspace_bytes(bad, 4, 4) == 0
     assert fo.int8_workspace_bytes(4, 4, 131072) == 0
