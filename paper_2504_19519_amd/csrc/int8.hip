@@ -30,7 +30,7 @@ namespace {
 // of the current one run, one barrier per step. An operand row of a step is 128 bytes,
 // chunk c of row r at slot c ^ ((r / 2) % 8): 16 rows' chunks lie on different banks.
 template <int DT, int BM, int BN, int ST, bool EXPERTS>
-__global__ __launch_bounds__(256, BM == 32 ? 4 : 2) void int8_block_kernel(const Int8Args a) {
+__global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 ? 1 : 2) void int8_block_kernel(const Int8Args a) {
     constexpr int kWaves = 4, WTM = BM / 2, WTN = BN / 2, MI = WTM / 16, NJ = WTN / 16;
     constexpr int kA = BM * 128, kStage = (BM + BN) * 128;
     constexpr int kAI = kA / 1024 / kWaves, kBI = BN * 128 / 1024 / kWaves, kLoads = kAI + kBI;

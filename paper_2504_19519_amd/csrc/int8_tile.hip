@@ -28,24 +28,33 @@ __device__ __forceinline__ void mfma_tied(i32x4_t& c, const u32x4_t& x, const u3
     else asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(x), "v"(y));
 }
 
-template <int DT, bool EXPERTS>
-__global__ __launch_bounds__(256, 1) void int8_tile_kernel(const Int8Args a) {
-    constexpr int BM = 256, BN = 256, WT = 128, MI = 8, NJ = 8;
-    constexpr int kA = BM * 128, kStage = (BM + BN) * 128;
-    constexpr int kHalf = 8, kLoads = 16;                // load instructions of A, and of both, per wave and step
-    constexpr int kVRows = 2;                            // accumulator block rows held in VGPRs
+// What a workgroup has in LDS: the two stages, and what the epilogue wants to know of the
+// tile's columns and rows. (The stages are separate arrays, so that the compiler can tell
+// the stage being read from the stage being filled.)
+constexpr int kStage = (256 + 256) * 128;
+struct Shared {
+    char* st0;
+    char* st1;
+    float* scale;
+    float* bias;
+    float* row;
+    bool* there;
+};
 
-    // the stages live in separate arrays, so that the compiler can tell the stage being
-    // read from the stage being filled
-    __shared__ __attribute__((aligned(1024))) char st0[kStage];
-    __shared__ __attribute__((aligned(1024))) char st1[kStage];
-    __shared__ __attribute__((aligned(16))) float s_scale[BN], s_bias[BN], s_row[BM];
-    __shared__ bool s_there[BM];
+// A tile of 256 rows, waves 2 x 2 of 128 x 128; or (HALF) of the up to 128 that are left,
+// waves side by side of 128 x 64.
+template <int DT, bool EXPERTS, bool HALF>
+__device__ __forceinline__ void tile_body(const Int8Args& a, const Block& b, const Shared& s) {
+    constexpr int BM = HALF ? 128 : 256, BN = 256, MI = 8, NJ = HALF ? 4 : 8;
+    constexpr int kA = BM * 128;
+    constexpr int kAI = BM / 32, kBI = BN / 32, kLoads = kAI + kBI;      // load instructions per wave and step
+    constexpr int kGap = MI * NJ / kLoads;               // MFMAs to a load
+    constexpr int kVRows = 2;                            // accumulator block rows held in VGPRs
+    char* const st0 = s.st0;
+    char* const st1 = s.st1;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave >> 1, wn = wave & 1;
-    Block b;
-    if (!find_block<BM, EXPERTS>(a, blockIdx.x, BN, b)) return;
+    const int row_w = HALF ? 0 : wave / 2 * 128, col_w = HALF ? wave * 64 : wave % 2 * 128;     // the wave's part
     const uint32_t bytes = (uint32_t)int8_row_bytes(a.K);
     const int steps = (int)((bytes + 127) / 128);
     const bool gather = EXPERTS && a.pair_of;
@@ -63,10 +72,10 @@ __global__ __launch_bounds__(256, 1) void int8_tile_kernel(const Int8Args a) {
     for (int i = 0; i < 2; ++i) place[i] = 16u * (uint32_t)((lane & 7) ^ ((4 * i + lane / 16) & 7));
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-        const int r = (wave * kHalf + i % kHalf) * 8 + lane / 8;
-        if (i < kHalf) {
-            const int64_t s = source_row<EXPERTS>(a, b, r);
-            voff[i] = s < 0 ? kOutside : (uint32_t)((gather ? s : r) * a.lda) + place[i & 1];
+        const int r = (i < kAI ? wave * kAI + i : wave * kBI + i - kAI) * 8 + lane / 8;
+        if (i < kAI) {
+            const int64_t from = source_row<EXPERTS>(a, b, r);
+            voff[i] = from < 0 ? kOutside : (uint32_t)((gather ? from : r) * a.lda) + place[i & 1];
         } else {
             voff[i] = r < cols ? (uint32_t)(r * a.ldb) + place[i & 1] : kOutside;
         }
@@ -78,23 +87,23 @@ __global__ __launch_bounds__(256, 1) void int8_tile_kernel(const Int8Args a) {
         constexpr int i = decltype(ic)::value;
         const uint32_t at = 128u * (uint32_t)t;
         const uint32_t v = place[i & 1] + at < bytes ? voff[i] : kOutside;
-        if constexpr (i < kHalf)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void_t*)(st + (wave * kHalf + i) * 1024), 16, v, at, 0, 0);
+        if constexpr (i < kAI)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void_t*)(st + (wave * kAI + i) * 1024), 16, v, at, 0, 0);
         else
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void_t*)(st + kA + (wave * kHalf + i - kHalf) * 1024), 16, v, at, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void_t*)(st + kA + (wave * kBI + i - kAI) * 1024), 16, v, at, 0, 0);
     };
 
     // Fragments: lane l feeds row l % 16 of a 16-row block with chunk 4 h + l / 16 of MFMA
     // substep h. The weights are the first operand: each lane holds four consecutive columns
     // of a row of c.
-    const int a_row = (wm * WT + (lane & 15)) * 128, b_row = kA + (wn * WT + (lane & 15)) * 128;
+    const int a_row = (row_w + (lane & 15)) * 128, b_row = kA + (col_w + (lane & 15)) * 128;
     int cslot[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) cslot[h] = 16 * ((4 * h + (lane >> 4)) ^ ((lane >> 1) & 7));
     i32x4_t acc[MI][NJ];
     u32x4_t fa0[MI], fb0[NJ], fa1[MI], fb1[NJ];
     // MFMA m of a substep carries fragment read m of the next one (the order in which that
-    // needs them) and, with `loads`, every fourth one a load of the stage just freed.
+    // needs them) and, with `loads`, every kGap-th one a load of the stage just freed.
     auto substep = [&](const u32x4_t (&xa)[MI], const u32x4_t (&xb)[NJ], const char* rst, auto h_next, u32x4_t (&ya)[MI],
                        u32x4_t (&yb)[NJ], auto loads, int t, char* lst, auto first) __attribute__((always_inline)) {
         constexpr int h = decltype(h_next)::value;
@@ -103,7 +112,8 @@ __global__ __launch_bounds__(256, 1) void int8_tile_kernel(const Int8Args a) {
             if constexpr (m == 0) ya[0] = *reinterpret_cast<const u32x4_t*>(rst + a_row + cslot[h]);
             else if constexpr (m <= NJ) yb[m - 1] = *reinterpret_cast<const u32x4_t*>(rst + b_row + (m - 1) * 2048 + cslot[h]);
             else if constexpr (m < MI + NJ) ya[m - NJ] = *reinterpret_cast<const u32x4_t*>(rst + a_row + (m - NJ) * 2048 + cslot[h]);
-            if constexpr (decltype(loads)::value && m % 4 == 0) load_one(std::integral_constant<int, m / 4>{}, t, lst);
+            if constexpr (decltype(loads)::value && m % kGap == 0 && m / kGap < kLoads)
+                load_one(std::integral_constant<int, m / kGap>{}, t, lst);
             mfma_tied<decltype(first)::value, (i >= MI - kVRows)>(acc[i][j], xb[j], xa[i]);
             __builtin_amdgcn_sched_barrier(0);
         });
@@ -122,10 +132,10 @@ __global__ __launch_bounds__(256, 1) void int8_tile_kernel(const Int8Args a) {
         substep(fa0, fb0, cur, k1, fa1, fb1, kNo, 0, cur, first);
         wait_and_barrier<0>();
         if constexpr (decltype(first)::value) {
-            s_scale[tid] = col_scale;
-            s_bias[tid] = col_bias;
-            s_row[tid] = row_scale;
-            s_there[tid] = there;
+            s.scale[tid] = col_scale;
+            s.bias[tid] = col_bias;
+            s.row[tid] = row_scale;
+            s.there[tid] = there;
         }
         substep(fa1, fb1, nxt, k0, fa0, fb0, kYes, t + 2, cur, kNo);
     };
@@ -133,9 +143,9 @@ __global__ __launch_bounds__(256, 1) void int8_tile_kernel(const Int8Args a) {
     static_for<kLoads>([&](auto ic) __attribute__((always_inline)) { load_one(ic, 0, st0); });
     static_for<kLoads>([&](auto ic) __attribute__((always_inline)) { load_one(ic, 1, st1); });
     {
-        const int64_t s = source_row<EXPERTS>(a, b, tid);
-        there = s >= 0;
-        if (there) row_scale = a.a_scales[s];
+        const int64_t from = source_row<EXPERTS>(a, b, tid);
+        there = from >= 0;
+        if (there) row_scale = a.a_scales[from];
         if (tid < cols) {
             const int64_t at = (int64_t)b.expert * a.N + b.col0 + tid;
             col_scale = a.b_scales[at];
@@ -166,20 +176,20 @@ __global__ __launch_bounds__(256, 1) void int8_tile_kernel(const Int8Args a) {
     int tid_e = tid;
     asm volatile("" : "+v"(tid_e)); // the epilogue's addresses are formed here, not ahead of the main loop
     const int lane_e = tid_e & 63, lr = lane_e & 15, lh = (lane_e >> 4) & 1, lq = lane_e >> 5;
-    char* const sb = wm == 0 ? st0 : st1;
+    char* const sb = row_w == 0 ? st0 : st1;
     static_for<NJ>([&](auto jc) __attribute__((always_inline)) {
         constexpr int j = decltype(jc)::value;
-        const int col = wn * WT + j * 16 + 4 * (lane_e >> 4);
-        const f32x4_t scale = *reinterpret_cast<const f32x4_t*>(s_scale + col);
-        const f32x4_t bias = *reinterpret_cast<const f32x4_t*>(s_bias + col);
+        const int col = col_w + j * 16 + 4 * (lane_e >> 4);
+        const f32x4_t scale = *reinterpret_cast<const f32x4_t*>(s.scale + col);
+        const f32x4_t bias = *reinterpret_cast<const f32x4_t*>(s.bias + col);
         static_for<MI>([&](auto ic) __attribute__((always_inline)) {
             constexpr int i = decltype(ic)::value;
-            const float row = s_row[wm * WT + i * 16 + lr];
+            const float row = s.row[row_w + i * 16 + lr];
             float v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = (float)acc[i][j][e] * row * scale[e] + bias[e];
             const u32x2_t w = {pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
-            const int r = i * 16 + lr, c = wn * 16 + 2 * j + lq;
+            const int r = i * 16 + lr, c = col_w / 8 + 2 * j + lq;
             *reinterpret_cast<u32x2_t*>(sb + r * 512 + ((c ^ (r & 31)) << 4) + 8 * lh) = w;
         });
     });
@@ -188,12 +198,25 @@ __global__ __launch_bounds__(256, 1) void int8_tile_kernel(const Int8Args a) {
     const int64_t left = cols - 8 * c;
     uint16_t* const out = a.c + b.row0 * a.ldc + b.col0 + 8 * c;
 #pragma unroll 8
-    for (int k = 0; k < 32; ++k) {
+    for (int k = 0; k < BM / 8; ++k) {
         const int r = r0 + 8 * k;
         const char* const from = (k < 16 ? st0 : st1) + (r & 127) * 512 + ((c ^ (r & 31)) << 4);
         const u32x4_t v = *reinterpret_cast<const u32x4_t*>(from);
-        if (s_there[r]) write_chunk(out + (int64_t)r * a.ldc, v, left);
+        if (s.there[r]) write_chunk(out + (int64_t)r * a.ldc, v, left);
     }
+}
+
+template <int DT, bool EXPERTS>
+__global__ __launch_bounds__(256, 1) void int8_tile_kernel(const Int8Args a) {
+    __shared__ __attribute__((aligned(1024))) char st0[kStage];
+    __shared__ __attribute__((aligned(1024))) char st1[kStage];
+    __shared__ __attribute__((aligned(16))) float s_scale[256], s_bias[256], s_row[256];
+    __shared__ bool s_there[256];
+    Block b;
+    if (!find_block<256, EXPERTS>(a, blockIdx.x, 256, b)) return;
+    const Shared s = {st0, st1, s_scale, s_bias, s_row, s_there};
+    if (b.rows > 128) tile_body<DT, EXPERTS, false>(a, b, s);
+    else tile_body<DT, EXPERTS, true>(a, b, s);
 }
 
 }  // namespace
