@@ -71,28 +71,30 @@ __device__ __forceinline__ float first_max(float v) {
     return bit_cast<float>(__builtin_amdgcn_readlane(bit_cast<int>(v), W - 1));
 }
 
-// The chunks of eight of a row of n values: chunk c of the last one's index `last`
-// starts at column 8 c, the last one at n - 8 (so that `twice` of its values are the
-// chunk's before it as well). Rows of fewer than eight values have one, read in parts.
+// The chunks of eight of a row of n values: chunk c starts at column 8 c, the last one at
+// n - 8 (so that `twice` of its values are the chunk's before it as well). SMALL: rows of
+// fewer than eight values, which have one, read and written in parts.
+template <bool SMALL>
 struct RowChunks {
     int n, last, twice;
     __device__ __forceinline__ explicit RowChunks(int64_t N)
-        : n((int)N), last(((int)N - 1) >> 3), twice(N < 8 ? 0 : 8 * (last + 1) - (int)N) {}
-    __device__ __forceinline__ int column(int c) const { return c == last && n >= 8 ? n - 8 : 8 * c; }
+        : n((int)N), last(((int)N - 1) >> 3), twice(SMALL ? 0 : 8 * (last + 1) - (int)N) {}
+    // (unsigned, so that an access takes a row's address from scalar registers)
+    __device__ __forceinline__ uint32_t column(int c) const { return (uint32_t)(8 * c - (c == last ? twice : 0)); }
     __device__ __forceinline__ u32x4_t read(const uint16_t* row, int c) const {
         if (c > last) return u32x4_t{0u, 0u, 0u, 0u};
-        return n >= 8 ? load8(row + column(c)) : read_chunk<kCached>(row, n);
+        return SMALL ? read_chunk<kCached>(row, n) : load8(row + column(c));
     }
     __device__ __forceinline__ void write(uint16_t* row, int c, u32x4_t v) const {
         if (c > last) return;
-        if (n >= 8) stream8(row + column(c), v);
-        else write_chunk(row, v, n);
+        if constexpr (SMALL) write_chunk(row, v, n);
+        else stream8(row + column(c), v);
     }
     // The sum over a chunk's values of their own, of term(e).
     template <typename F>
     __device__ __forceinline__ float sum(int c, F term) const {
         float s = 0.0f;
-        if (twice == 0) {
+        if (SMALL || twice == 0) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) s += term(e);
         } else {
@@ -106,34 +108,48 @@ struct RowChunks {
 
 // What turns a row's values into codes. m: the row's largest magnitude.
 struct RowCodes {
-    float up, inverse, m;       // values times `up` (a power of two) times `inverse` (127 / (m up)) is nearly 127 t / m
+    float inverse, m;           // 127 / m, within 2^-22 of it; of values and m times `by`
+    float by;                   // 1, but for an m whose reciprocal is not a normal number (or nearly so)
     bool finite;
     __device__ __forceinline__ explicit RowCodes(float m_) : m(m_) {
-        up = m < 0x1p-60f ? 0x1p64f : 1.0f;
+        by = m < 0x1p-100f ? 0x1p64f : m > 0x1p100f ? 0x1p-64f : 1.0f;
         finite = m < __builtin_inff();
-        inverse = m > 0.0f && finite ? 127.0f / (m * up) : 0.0f;
+        inverse = m > 0.0f && finite ? 127.0f * __builtin_amdgcn_rcpf(m * by) : 0.0f;
     }
 };
 
+// v / 127, rounded once: the error of the product with 1 / 127 taken back.
+__device__ __forceinline__ float over_127(float v) {
+    constexpr float kInverse = 1.0f / 127.0f;
+    if (v < 0x1p-100f) return v / 127.0f;
+    const float q = v * kInverse;
+    return __builtin_fmaf(__builtin_fmaf(-q, 127.0f, v), kInverse, q);
+}
+
 // 127 t / m to the nearest whole number, ties to even, in eight codes' low bytes. The
-// product with the reciprocal is off by less than 2^-16: where it comes so near to a
-// tie that this could decide, 127 t is compared with the tie in 64 bits, in which both
-// are exact (t has at most 22 bits, m as many).
+// product with the reciprocal is off by less than 2^-15: where it comes so near to a tie
+// that this could decide, 127 t is compared with the tie in 64 bits, in which both are
+// exact (t has at most 22 bits, m as many).
 __device__ __forceinline__ u32x2_t codes_of(const float* t, const RowCodes& r) {
     constexpr float kWhole = 12582912.0f;          // 1.5 * 2^23: adding it rounds to a whole number
-    float q[8], w[8];
-    bool near = false;
+    constexpr float kNear = 0.5f - 0x1p-15f;
+    float v[8], w[8], most = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = t[e];
+    if (r.by != 1.0f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= r.by;
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        q[e] = t[e] * r.up * r.inverse;
-        w[e] = q[e] + kWhole;
-        near = near || __builtin_fabsf(q[e] - (w[e] - kWhole)) > 0.5f - 0x1p-15f;
+        w[e] = __builtin_fmaf(v[e], r.inverse, kWhole);
+        most = __builtin_fmaxf(most, __builtin_fabsf(__builtin_fmaf(v[e], r.inverse, kWhole - w[e])));
     }
-    if (near) {
+    if (most > kNear) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float c = w[e] - kWhole, off = q[e] - c;
-            if (__builtin_fabsf(off) > 0.5f - 0x1p-15f) {
+            const float c = w[e] - kWhole, off = __builtin_fmaf(v[e], r.inverse, -c);
+            if (__builtin_fabsf(off) > kNear) {
                 const float low = off > 0.0f ? c : c - 1.0f;        // the tie is low + 1/2
                 const double d = 127.0 * (double)t[e] - ((double)low + 0.5) * (double)r.m;
                 const bool odd = ((int)low & 1) != 0;
@@ -153,16 +169,17 @@ __device__ __forceinline__ u32x2_t codes_of(const float* t, const RowCodes& r) {
 
 // A chunk's codes to their places; the last chunk also clears what is behind the row's
 // end, up to a multiple of 16.
-__device__ __forceinline__ void write_codes(int8_t* row, int c, const RowChunks& k, u32x2_t code) {
+template <bool SMALL>
+__device__ __forceinline__ void write_codes(int8_t* row, int c, const RowChunks<SMALL>& k, u32x2_t code) {
     if (c > k.last) return;
     if (c == k.last) {
         uint64_t v = (uint64_t)code[1] << 32 | code[0];
         v >>= 8 * k.twice;                         // the chunk's own values first, zeros behind them
         code[0] = (uint32_t)v;
         code[1] = (uint32_t)(v >> 32);
-        if ((c & 1) == 0) *reinterpret_cast<u32x2_t*>(row + 8 * (int64_t)c + 8) = u32x2_t{0u, 0u};
+        if ((c & 1) == 0) *reinterpret_cast<u32x2_t*>(row + 8 * (uint32_t)c + 8) = u32x2_t{0u, 0u};
     }
-    *reinterpret_cast<u32x2_t*>(row + 8 * (int64_t)c) = code;
+    *reinterpret_cast<u32x2_t*>(row + 8 * (uint32_t)c) = code;
 }
 
 constexpr int group_rows(int threads) { return threads < 64 ? 64 / threads : 1; }
@@ -170,12 +187,12 @@ constexpr int group_rows(int threads) { return threads < 64 ? 64 / threads : 1; 
 // TH threads to a row, CH chunks each, a wave on several rows where they are short. The
 // next row's loads are issued ahead of this row's sums. NORM: the sum's norm; else the
 // codes of x.
-template <int DT, int CH, int TH, bool NORM>
+template <int DT, int CH, int TH, bool NORM, bool SMALL>
 __global__ __launch_bounds__(TH < 64 ? 64 : TH, 4) void rows8_kernel(const Rows8Args a) {
     constexpr int ROWS = group_rows(TH), kRowWaves = TH / 64;
     __shared__ float s_join[2][2][kRowWaves > 1 ? kRowWaves : 1];
     const int lane = threadIdx.x % TH, group = row_group<TH>();
-    const RowChunks k(a.N);
+    const RowChunks<SMALL> k(a.N);
     const int64_t step = (int64_t)gridDim.x * ROWS;
     const float inv_n = 1.0f / ((float)a.N * a.scale);
 
@@ -205,11 +222,21 @@ __global__ __launch_bounds__(TH < 64 ? 64 : TH, 4) void rows8_kernel(const Rows8
     load(i);
     for (int64_t round = 0; round < rounds; ++round, i += step) {
         u32x4_t v[CH];              // x, or h
+        // x, or h gamma: kept for the output where the registers suffice, else formed again
+        constexpr bool kKeep = !NORM || CH <= 3;
+        float kept[kKeep ? CH : 1][8];
+        auto scaled = [&](int t, float* x) {
+            float g[8];
+            asm volatile("" : "+v"(gamma[NORM ? t : 0]));      // widened anew for each row: half the registers
+            widen<DT>(gamma[NORM ? t : 0], g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= g[e];
+        };
         float square = 0.0f, m = 0.0f;
 #pragma unroll
         for (int t = 0; t < CH; ++t) {
             v[t] = next[t];
-            float x[8];
+            float* const x = kept[kKeep ? t : 0];
             if constexpr (NORM) {
                 if (a.residual) {
                     float r[8];
@@ -223,12 +250,7 @@ __global__ __launch_bounds__(TH < 64 ? 64 : TH, 4) void rows8_kernel(const Rows8
             widen<DT>(v[t], x);
             if constexpr (NORM) {
                 square += k.sum(lane + TH * t, [&](int e) { return x[e] * x[e]; });
-                if (a.codes) {
-                    float g[8];
-                    widen<DT>(gamma[t], g);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] *= g[e];
-                }
+                scaled(t, x);
             }
             if (!NORM || a.codes) m = __builtin_elementwise_maximum(m, top_of(x));
         }
@@ -255,29 +277,25 @@ __global__ __launch_bounds__(TH < 64 ? 64 : TH, 4) void rows8_kernel(const Rows8
             if constexpr (NORM) {
                 if (a.rstd) a.rstd[i] = rstd;
             }
-            if (a.codes) a.scales[i] = codes.finite ? m * rstd / 127.0f : __builtin_nanf("");
+            if (a.codes) a.scales[i] = codes.finite ? over_127(m * rstd) : __builtin_nanf("");
         }
 #pragma unroll
         for (int t = 0; t < CH; ++t) {
             const int c = lane + TH * t;
-            float x[8];
+            float* const x = kept[kKeep ? t : 0];
+            if constexpr (!kKeep) {
+                asm volatile("" : "+v"(v[t]));
+                widen<DT>(v[t], x);
+                if constexpr (NORM) scaled(t, x);
+            }
             if constexpr (NORM) {
                 if (a.h) k.write(a.h + i * a.ldh, c, v[t]);
-                float g[8];
-                asm volatile("" : "+v"(gamma[t]), "+v"(v[t]));      // widened anew: half the registers
-                widen<DT>(v[t], x);
-                widen<DT>(gamma[t], g);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] *= g[e];
                 if (a.y) {
                     float y[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[e] = x[e] * rstd;
                     k.write(a.y + i * a.ldy, c, narrow<DT>(y));
                 }
-            } else {
-                asm volatile("" : "+v"(v[t]));
-                widen<DT>(v[t], x);
             }
             if (!NORM || a.codes) write_codes(a.codes + i * a.ldc, c, k, codes_of(x, codes));
         }
@@ -290,7 +308,7 @@ constexpr int kLongThreads = 1024;
 template <int DT>
 __global__ __launch_bounds__(kLongThreads) void quantize_long_kernel(const Rows8Args a) {
     __shared__ float s_max[kLongThreads / 64];
-    const RowChunks k(a.N);
+    const RowChunks<false> k(a.N);
     for (int64_t i = blockIdx.x; i < a.M; i += gridDim.x) {
         const uint16_t* row = a.x + i * a.ldx;
         float m = 0.0f;
@@ -304,7 +322,7 @@ __global__ __launch_bounds__(kLongThreads) void quantize_long_kernel(const Rows8
         __syncthreads();
         m = first_max<16>((threadIdx.x & 63) < 16 ? s_max[threadIdx.x & 63] : 0.0f);
         const RowCodes codes(m);
-        if (threadIdx.x == 0) a.scales[i] = codes.finite ? m / 127.0f : __builtin_nanf("");
+        if (threadIdx.x == 0) a.scales[i] = codes.finite ? over_127(m) : __builtin_nanf("");
         for (int c = threadIdx.x; c <= k.last; c += kLongThreads) {
             float x[8];
             widen<DT>(k.read(row, c), x);
@@ -324,13 +342,13 @@ struct GradPart {
 
 // ROWS rows at a time, TH threads each; every thread keeps its columns' sums of
 // dy h r over all of its rows, and the next AHEAD rows' loads are in flight.
-template <int DT, int CH, int TH, int ROWS, int AHEAD>
+template <int DT, int CH, int TH, int ROWS, int AHEAD, bool SMALL>
 __global__ __launch_bounds__(TH * ROWS) void norm_add_backward_kernel(const NormAddArgs a) {
     constexpr int kWaves = TH * ROWS / 64, kRowWaves = TH / 64;
     __shared__ float s_sum[2][kWaves];
     __shared__ float s_cols[ROWS > 1 ? ROWS / 2 : 1][ROWS > 1 ? 8 * CH : 1][ROWS > 1 ? TH : 1];
     const int lane = threadIdx.x % TH, group = row_group<TH>();
-    const RowChunks k(a.N);
+    const RowChunks<SMALL> k(a.N);
     const int64_t step = (int64_t)gridDim.x * ROWS;
     const float inv_n = 1.0f / (float)a.N;
 
@@ -453,7 +471,7 @@ constexpr int kWideThreads = 256;
 template <int DT>
 __global__ __launch_bounds__(1024) void norm_add_wide_dots_kernel(const NormAddArgs a) {
     __shared__ float s_sum[2][16];
-    const RowChunks k(a.N);
+    const RowChunks<false> k(a.N);
     int set = 0;
     for (int64_t i = blockIdx.x; i < a.M; i += gridDim.x, set ^= 1) {
         float s = 0.0f;
@@ -573,11 +591,20 @@ template <bool NORM>
 static hipError_t launch_rows8(int dtype, const Rows8Args& a, hipStream_t s) {
     return for_form(a.N, [&](auto th, auto ch) {
         constexpr int TH = decltype(th)::value, CH = decltype(ch)::value, kThreads = TH < 64 ? 64 : TH;
-        // sixteen waves to a compute unit of 256
-        const int64_t rows = group_rows(TH), most = 4096 * 64 / kThreads;
-        const uint32_t blocks = (uint32_t)std::min<int64_t>((a.M + rows - 1) / rows, most);
-        return launch(dtype == FO_FP16 ? rows8_kernel<FO_FP16, CH, TH, NORM> : rows8_kernel<FO_BF16, CH, TH, NORM>, blocks,
-                      kThreads, s, a);
+        // Waves over all compute units (256): the more of a row they have in flight each, the
+        // fewer. (us: 8192x8192 bf16 to codes with 2048, 4096 and 8192 waves 66, 44, 41; its
+        // norm and the backward pass 189, 193, 193; 4096x4096 to codes by the norm 29.3, 27.6,
+        // 28.2.)
+        const int64_t rows = group_rows(TH), groups = (a.M + rows - 1) / rows;
+        const int64_t waves = !NORM ? 8192 : groups * kThreads / 64 >= 16 * 2048 ? 2048 : 4096;
+        const uint32_t blocks = (uint32_t)std::min<int64_t>(groups, waves * 64 / kThreads);
+        if constexpr (TH == 8 && CH == 1) {
+            if (a.N < 8)
+                return launch(dtype == FO_FP16 ? rows8_kernel<FO_FP16, CH, TH, NORM, true> : rows8_kernel<FO_BF16, CH, TH, NORM, true>,
+                              blocks, kThreads, s, a);
+        }
+        return launch(dtype == FO_FP16 ? rows8_kernel<FO_FP16, CH, TH, NORM, false> : rows8_kernel<FO_BF16, CH, TH, NORM, false>,
+                      blocks, kThreads, s, a);
     });
 }
 
@@ -607,8 +634,14 @@ hipError_t launch_norm_add_backward(int dtype, const NormAddArgs& a, float* dgam
             constexpr int CH = decltype(ch)::value, TH = decltype(th)::value, ROWS = decltype(rows)::value;
             constexpr int AHEAD = 1;
             blocks = std::min<int64_t>((a.M + ROWS - 1) / ROWS, 256);
-            return launch(dtype == FO_FP16 ? norm_add_backward_kernel<FO_FP16, CH, TH, ROWS, AHEAD>
-                                           : norm_add_backward_kernel<FO_BF16, CH, TH, ROWS, AHEAD>,
+            if constexpr (TH == 8) {
+                if (a.N < 8)
+                    return launch(dtype == FO_FP16 ? norm_add_backward_kernel<FO_FP16, CH, TH, ROWS, AHEAD, true>
+                                                   : norm_add_backward_kernel<FO_BF16, CH, TH, ROWS, AHEAD, true>,
+                                  (uint32_t)blocks, TH * ROWS, s, a);
+            }
+            return launch(dtype == FO_FP16 ? norm_add_backward_kernel<FO_FP16, CH, TH, ROWS, AHEAD, false>
+                                           : norm_add_backward_kernel<FO_BF16, CH, TH, ROWS, AHEAD, false>,
                           (uint32_t)blocks, TH * ROWS, s, a);
         });
     }
