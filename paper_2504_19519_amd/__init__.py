@@ -727,32 +727,34 @@ class _Args:
             self._place(d, what)
         if x.dtype not in (_TYPES or _types())["u8"]:
             raise ValueError(f"{what}: {x.dtype} values for 8-bit codes")
-        if ld is not None or x.dim() < 2 or M == 0 or N == 0:
+        shape = x.shape
+        if ld is not None or len(shape) < 2 or M == 0 or N == 0:
             ld = width if ld is None else int(ld)
             if not x.is_contiguous() or x.numel() < ((M - 1) * ld + width if M > 0 and N > 0 else 0):
                 raise ValueError(f"{what}: contiguous codes are needed, {M} rows of {width} bytes, {ld} apart")
             return x.data_ptr(), ld
-        shape = x.shape
-        length = shape[-1]
+        if len(shape) == 2:
+            (have, length), (step, unit) = shape, x.stride()
+            if length == width and unit == 1 and have >= M > 1 and step >= width:
+                return x.data_ptr(), step
+        elif x.is_contiguous():
+            length = shape[-1]
+            have, step, unit = x.numel() // max(length, 1), length, 1
+        else:
+            raise ValueError(f"{what}: more than two dimensions have to be contiguous")
         if length != N and length != width:
             raise ValueError(f"{what}: shape {tuple(shape)} for rows of {N}: a [{M}, {N}] or [{M}, {width}] view or a row "
                              f"distance is needed")
-        if x.dim() == 2:
-            have, (step, unit) = shape[0], x.stride()
-        elif x.is_contiguous():
-            have, step, unit = x.numel() // length, length, 1
-        else:
-            raise ValueError(f"{what}: more than two dimensions have to be contiguous")
         if have < M:
             raise ValueError(f"{what}: {have} rows, the call needs {M}")
         if M == 1:
-            step = max(step, width)
+            step = width
         if (unit != 1 and length > 1) or step < width:
             raise ValueError(f"{what}: rows of unit stride, at least {width} bytes apart, are needed; strides are "
                              f"{tuple(x.stride())}")
         if length < width and x.storage_offset() + (M - 1) * step + width > x.untyped_storage().nbytes():
             raise ValueError(f"{what}: the last row's codes end at {width} bytes, behind the tensor's memory")
-        return x.data_ptr(), step if M > 1 else width
+        return x.data_ptr(), step
 
     def pack(self, packed, scales, M: int, N: int, fmt):
         """(packed, scales, format) of an [M, N] checkpoint."""

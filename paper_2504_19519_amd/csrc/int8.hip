@@ -62,6 +62,28 @@ __global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 ? 1 : 2) void int8_bloc
 
     const bool gather = EXPERTS && a.pair_of;
     const int8_t* const ablk = gather ? a.a : a.a + b.row0 * a.lda;
+
+    // What the epilogue wants to know of the rows and columns, a row and a column to a thread:
+    // looked up ahead of the operands' loads, in LDS by the first steps.
+    __shared__ int s_from[EXPERTS ? BM : 1];             // row of a, or -1
+    __shared__ __attribute__((aligned(16))) float s_row[BM], s_scale[BN], s_bias[BN];
+    const int tid = threadIdx.x;
+    float row_scale = 0.0f, col_scale = 0.0f, col_bias = 0.0f;
+    if (tid < BM) {
+        const int64_t from = source_row<EXPERTS>(a, b, tid);
+        if constexpr (EXPERTS) s_from[tid] = (int)from;
+        if (from >= 0) row_scale = a.a_scales[from];
+    }
+    auto look_up = [&]() {
+        const int64_t n = b.col0 + tid, at = (int64_t)b.expert * a.N + n;
+        if (tid < BN && n < a.N) {
+            col_scale = a.b_scales[at];
+            if (a.bias) col_bias = to_f32<DT>(a.bias[at]);
+        }
+    };
+    look_up();
+    if constexpr (EXPERTS) wait_and_barrier<63>();
+
     // A load instruction fills 1 KB: 8 operand rows of 128 bytes. A lane's offset from the
     // operand's base, or kOutside for a row that is not there; and its place in the row.
     uint32_t voff[kLoads], place[kLoads];
@@ -70,8 +92,8 @@ __global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 ? 1 : 2) void int8_bloc
         const int r = (i < kAI ? wave * kAI + i : wave * kBI + i - kAI) * 8 + lane / 8;
         place[i] = 16u * (uint32_t)((lane & 7) ^ ((r >> 1) & 7));
         if (i < kAI) {
-            const int64_t s = source_row<EXPERTS>(a, b, r);
-            voff[i] = s < 0 ? kOutside : (uint32_t)((gather ? s : r) * a.lda) + place[i];
+            const int from = EXPERTS ? s_from[EXPERTS ? r : 0] : r < b.rows ? r : -1;
+            voff[i] = from < 0 ? kOutside : (uint32_t)((gather ? from : r) * a.lda) + place[i];
         }
     }
     // Fragments: lane l feeds row l % 16 of a 16-row block with chunk 4 h + l / 16 of MFMA
@@ -82,14 +104,33 @@ __global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 ? 1 : 2) void int8_bloc
 #pragma unroll
     for (int h = 0; h < 2; ++h) cslot[h] = 16 * ((4 * h + (lane >> 4)) ^ ((lane >> 1) & 7));
     const int64_t end = a.N - b.col0 < (int64_t)BN * a.span ? a.N : b.col0 + BN * a.span;
-    do {
-        const int8_t* const bblk = a.b + ((int64_t)b.expert * a.N + b.col0) * a.ldb;
-        const int cols = (int)(a.N - b.col0 < BN ? a.N - b.col0 : BN);
+    const int8_t* bblk;
+    auto load_at = [&](auto ic, int t, char* st) __attribute__((always_inline)) {
+        constexpr int i = decltype(ic)::value;
+        constexpr bool is_a = i < kAI;
+        const __amdgpu_buffer_rsrc_t r =
+            __builtin_amdgcn_make_buffer_rsrc((void*)(is_a ? ablk : bblk), 0, (int)kSpan, kRsrcWord3);
+        // (the step's offset past kOutside stays outside)
+        const uint32_t at = 128u * (uint32_t)(first + t);
+        const uint32_t v = place[i] + at < (uint32_t)bytes ? voff[i] : kOutside;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            r, (lds_void_t*)(st + (is_a ? 0 : kA) + (is_a ? wave * kAI + i : wave * kBI + i - kAI) * 1024), 16, v, at, 0, 0);
+    };
+    // The first loads of the block at b.col0.
+    auto begin = [&]() __attribute__((always_inline)) {
+        bblk = a.b + ((int64_t)b.expert * a.N + b.col0) * a.ldb;
 #pragma unroll
         for (int i = kAI; i < kLoads; ++i) {
             const int r = (wave * kBI + i - kAI) * 8 + lane / 8;
-            voff[i] = r < cols ? (uint32_t)(r * a.ldb) + place[i] : kOutside;
+            voff[i] = r < a.N - b.col0 ? (uint32_t)(r * a.ldb) + place[i] : kOutside;
         }
+        static_for<ST>([&](auto uc) __attribute__((always_inline)) {
+            static_for<kLoads>([&](auto ic) __attribute__((always_inline)) { load_at(ic, decltype(uc)::value, stage(uc)); });
+        });
+    };
+    begin();
+    bool more;
+    do {
         u32x4_t fa[2][MI], fb[2][NJ];
         i32x4_t acc[MI][NJ];
 #pragma unroll
@@ -97,17 +138,6 @@ __global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 ? 1 : 2) void int8_bloc
 #pragma unroll
             for (int j = 0; j < NJ; ++j) acc[i][j] = i32x4_t{0, 0, 0, 0};
 
-        auto load_at = [&](auto ic, int t, char* st) __attribute__((always_inline)) {
-            constexpr int i = decltype(ic)::value;
-            constexpr bool is_a = i < kAI;
-            const __amdgpu_buffer_rsrc_t r =
-                __builtin_amdgcn_make_buffer_rsrc((void*)(is_a ? ablk : bblk), 0, (int)kSpan, kRsrcWord3);
-            // (the step's offset past kOutside stays outside)
-            const uint32_t at = 128u * (uint32_t)(first + t);
-            const uint32_t v = place[i] + at < (uint32_t)bytes ? voff[i] : kOutside;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                r, (lds_void_t*)(st + (is_a ? 0 : kA) + (is_a ? wave * kAI + i : wave * kBI + i - kAI) * 1024), 16, v, at, 0, 0);
-        };
         auto read_one = [&](auto ic, auto hc, const char* st, u32x4_t (&xa)[MI], u32x4_t (&xb)[NJ])
                             __attribute__((always_inline)) {
             constexpr int i = decltype(ic)::value, h = decltype(hc)::value;
@@ -158,10 +188,12 @@ __global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 ? 1 : 2) void int8_bloc
             }
         };
 
-        static_for<ST>([&](auto uc) __attribute__((always_inline)) {
-            static_for<kLoads>([&](auto ic) __attribute__((always_inline)) { load_at(ic, decltype(uc)::value, stage(uc)); });
-        });
         wait_and_barrier<(ST - 1) * kLoads>();
+        if (tid < BM) s_row[tid] = row_scale;
+        if (tid < BN) {
+            s_scale[tid] = col_scale;
+            s_bias[tid] = col_bias;
+        }
         static_for<MI + NJ>([&](auto ic) __attribute__((always_inline)) {
             read_one(ic, std::integral_constant<int, 0>{}, st0, fa[0], fb[0]);
         });
@@ -169,7 +201,7 @@ __global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 ? 1 : 2) void int8_bloc
         for (; t + ST <= steps; t += ST)
             static_for<ST>([&](auto uc) __attribute__((always_inline)) { step(uc, t + decltype(uc)::value); });
         rest(rest, std::integral_constant<int, 0>{}, t);
-        // (every wave has read the stages, and no load is writing LDS: the next block's loads, or the end)
+        // every wave has read the stages, and no load is writing LDS
         wait_and_barrier<0>();
 
         const int64_t col = b.col0 + wn * WTN;
@@ -187,35 +219,42 @@ __global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 ? 1 : 2) void int8_bloc
                         if (n < a.N) *reinterpret_cast<i32x4_t*>(to + n) = acc[i][j];
                     }
                 }
-                continue;
+                return;
             }
+        }
+        f32x4_t scale[NJ], bias[NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            scale[j] = *reinterpret_cast<const f32x4_t*>(s_scale + wn * WTN + 16 * j + 4 * (lane >> 4));
+            bias[j] = *reinterpret_cast<const f32x4_t*>(s_bias + wn * WTN + 16 * j + 4 * (lane >> 4));
+        }
+        more = EXPERTS && (b.col0 += BN) < end;
+        if (more) {                     // the next block's first loads ahead of this one's results
+            look_up();
+            begin();
         }
 
         // A wave's part of the block, 16 rows at a time: through LDS into whole rows.
-        Columns of[NJ];
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) of[j] = columns_of<DT>(a, b.expert, col + 16 * j + 4 * (lane >> 4));
         char* const out = s_out[wave];
         static_for<MI>([&](auto ic) __attribute__((always_inline)) {
             constexpr int i = decltype(ic)::value;
             const int r0 = wm * WTM + 16 * i;
-            const int64_t s = source_row<EXPERTS>(a, b, r0 + (lane & 15));
-            const float scale = s < 0 ? 0.0f : a.a_scales[s];
+            const float row = s_row[r0 + (lane & 15)];
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
                 *reinterpret_cast<u32x2_t*>(out + (lane & 15) * kOutRow + 32 * j + 8 * (lane >> 4)) =
-                    finish<DT>(acc[i][j], scale, of[j]);
+                    finish<DT>(acc[i][j], row, scale[j], bias[j]);
             constexpr int kChunks = WTN / 8;            // of a row
 #pragma unroll
             for (int q = 0; q < 16 * kChunks / 64 + (16 * kChunks % 64 != 0); ++q) {
                 const int at = 64 * q + lane, r = at / kChunks, ch = at % kChunks;
                 if (r >= 16) continue;
                 const u32x4_t v = *reinterpret_cast<const u32x4_t*>(out + r * kOutRow + 16 * ch);
-                if (source_row<EXPERTS>(a, b, r0 + r) < 0) continue;
+                if (EXPERTS ? s_from[EXPERTS ? r0 + r : 0] < 0 : r0 + r >= b.rows) continue;
                 write_chunk(a.c + (b.row0 + r0 + r) * a.ldc + col + 8 * ch, v, a.N - col - 8 * ch);
             }
         });
-    } while (EXPERTS && (b.col0 += BN) < end);
+    } while (more);
 }
 
 // ---- few blocks -------------------------------------------------------------
@@ -306,7 +345,8 @@ __global__ __launch_bounds__(256) void int8_few_kernel(const Int8Args a) {
     const int64_t n = b.col0 + 4 * (lane >> 4);
     if (wave != 0 || r >= b.rows || n >= a.N) return;
     const i32x4_t sum = (s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane]);
-    const u32x2_t v = finish<DT>(sum, a.a_scales[b.row0 + r], columns_of<DT>(a, 0, n));
+    const Columns of = columns_of<DT>(a, n);
+    const u32x2_t v = finish<DT>(sum, a.a_scales[b.row0 + r], of.scale, of.bias);
     write_four(a.c + (b.row0 + r) * a.ldc + n, v, a.N - n);
 }
 
@@ -320,7 +360,8 @@ __global__ __launch_bounds__(kJoinThreads) void int8_join_kernel(const Int8Args 
     const int64_t m = at / ld, n = at % ld;
     i32x4_t sum = {0, 0, 0, 0};
     for (int p = 0; p < a.parts; ++p) sum += *reinterpret_cast<const i32x4_t*>(a.partial + (int64_t)p * a.M * ld + at);
-    const u32x2_t v = finish<DT>(sum, a.a_scales[m], columns_of<DT>(a, 0, n));
+    const Columns of = columns_of<DT>(a, n);
+    const u32x2_t v = finish<DT>(sum, a.a_scales[m], of.scale, of.bias);
     write_four(a.c + m * a.ldc + n, v, a.N - n);
 }
 
@@ -355,39 +396,41 @@ int64_t blocks_ns(int64_t blocks, int64_t steps) {
     return blocks / 512 * (1030 * steps + 4000) + (rest == 0 ? 0 : rest <= 256 ? 700 * steps + 3000 : 1030 * steps + 4000);
 }
 
-// The form for what blocks(rows, cols) of each kind there are, `most` rows in the tallest.
-template <typename F>
-Form form_of(int64_t most, int64_t steps, F blocks) {
-    const int64_t b128 = blocks(128, 128), b32 = blocks(32, 32);
-    if (steps > 0 && most > 128 && tiles_ns(blocks(256, 256), steps) < blocks_ns(b128, steps)) return {256, 256, 2, 1, 1};
-    if (most > 40 && b128 >= 144) return {128, 128, b128 <= 256 ? 3 : 2, 1, 1};
-    if (most > 10 && b32 > 512) return {64, 64, 4, 1, 1};
-    return {32, 32, 4, 1, 1};
-}
+// us, bf16: 1024 x 4096 x 4096 in blocks of 128 with three stages 21, with two 25, of 64 28;
+// 512 x 4096 x 4096 of 64 16, of 128 25; 128 x 4096 x 4096 of 32 9.6, of 64 10.0, 256 x 4096
+// x 4096 15.5 and 10.6; 16 x 14336 x 4096 of 32 11.3, of 64 12.0. In parts: 16 x 256 x 16384
+// 8.7 for 16.0, 128 x 1024 x 16384 13.1 for 18.5, but 16 x 256 x 4096 6.7 for 6.4.
 Form product_form(int64_t M, int64_t N, int64_t K) {
     const int64_t steps = (int8_row_bytes(K) + 127) / 128;
-    Form f = form_of(M, steps, [&](int64_t rows, int64_t cols) { return ((M + rows - 1) / rows) * ((N + cols - 1) / cols); });
-    if (M <= 32 && f.rows == 64) f = {32, 32, 4, 1, 1};
-    if (f.rows == 32) {
-        const auto blocks = [&](int64_t size) { return ((M + size - 1) / size) * ((N + size - 1) / size); };
-        if (blocks(32) <= 128 && steps >= 64) f.parts = 4;
-        else if (blocks(16) <= 256) f = {16, 16, 0, 1, 1};
-    }
-    return f;
+    const auto blocks = [&](int64_t size) { return ((M + size - 1) / size) * ((N + size - 1) / size); };
+    if (M > 128 && K > 0 && tiles_ns(blocks(256), steps) < blocks_ns(blocks(128), steps)) return {256, 256, 2, 1, 1};
+    if (M > 40 && blocks(128) > 256) return {128, 128, 2, 1, 1};
+    if (M > 40 && blocks(128) >= 144 && steps >= 8) return {128, 128, 3, 1, 1};
+    if (M > 32 && blocks(32) > 512) return {64, 64, 4, 1, 1};
+    if (blocks(32) <= 128 && steps >= 64) return {32, 32, 4, 4, 1};
+    if (blocks(16) <= 256) return {16, 16, 0, 1, 1};
+    return {32, 32, 4, 1, 1};
 }
+
+// By experts, whose rows the host does not know: as if those that can have some had the same
+// number. Several blocks to a workgroup where the sums are short: it looks for its expert and
+// rows once, and a block's first loads go ahead of the results of the one before it. us, bf16,
+// blocks of 128 / 64 / 32 and how many to a workgroup:
+//   309 tokens to 8 of 256, 2934 columns  K 128   1: 56 / - / -  2: 45 / 63 / 69  4: 44 / 54 / 53
+//                                         K 1024  1: 145         2: 142 / 148 / 161  4: 153 / 145 / 150
+//   16 tokens to 8 of 256, 7168 columns   K 2048  1: 200 / 202   2: 191 / 185 / 195  4: 188 / 183 / 189
+//                          2048 columns   K 7168  1: 201 / 173 / 177  2: 230 / 179 / 183  4: - / 198 / 189
+//   512 tokens to 8 of 64, 2048 columns   K 2048  1: 70 / 79     2: 85 / 77 / 103
+//   1217 tokens to 4 of 60, 2881 columns  K 1409  1: 94 / 116    2: 95 / 115 / 154   (in tiles 110)
 Form experts_form(const Int8Args& a) {
     const int64_t pairs = a.pair_of ? std::min<int64_t>(a.capacity, a.a_rows * a.choices) : a.capacity;
     const int64_t experts = std::min<int64_t>(a.E, pairs), each = (pairs + experts - 1) / experts;
     const int64_t steps = (int8_row_bytes(a.K) + 127) / 128;
-    const auto blocks = [&](int64_t rows, int64_t cols) { return experts * ((each + rows - 1) / rows) * ((a.N + cols - 1) / cols); };
-    Form f = form_of(each, steps, blocks);
-    if (f.rows == 128) f.stages = 2;        // (how many blocks there are is not known here)
-    // Several blocks to a workgroup where they are short: it looks for its expert and rows once
-    // (256 experts, 10 rows each, 2934 columns: K 128 82 -> 60 us; 16 tokens to 8 of 256, 7168
-    // columns, K 2048 213 -> 195).
-    if (f.rows == 128 && steps <= 4) f.span = 2;
-    if (f.rows <= 64 && steps <= 16 && blocks(f.rows, f.cols) >= 4096) f.span = 4;
-    return f;
+    const auto blocks = [&](int64_t size) { return experts * ((each + size - 1) / size) * ((a.N + size - 1) / size); };
+    if (each > 192 && a.K > 0 && tiles_ns(blocks(256), steps) < blocks_ns(blocks(128), steps)) return {256, 256, 2, 1, 1};
+    if (each > 8 && blocks(128) >= 144) return {128, 128, 2, 1, blocks(128) < 2048 || steps > 8 ? 1 : steps > 2 ? 2 : 4};
+    if (blocks(32) > 2048 || (each > 8 && blocks(32) > 512)) return {64, 64, 4, 1, blocks(64) < 6000 || steps > 16 ? 1 : 4};
+    return {32, 32, 4, 1, 1};
 }
 
 template <int N>

@@ -135,27 +135,28 @@ __device__ __forceinline__ int64_t source_row(const Int8Args& a, const Block& b,
     }
 }
 
-// A row's four results of the columns n .. n + 3.
+// The scales and bias of columns n .. n + 3 (not by experts).
 struct Columns {
-    float scale[4], bias[4];
+    f32x4_t scale, bias;
 };
 template <int DT>
-__device__ __forceinline__ Columns columns_of(const Int8Args& a, int64_t expert, int64_t n) {
+__device__ __forceinline__ Columns columns_of(const Int8Args& a, int64_t n) {
     Columns c;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const bool there = n + e < a.N;
-        const int64_t at = expert * a.N + n + e;
-        c.scale[e] = there ? a.b_scales[at] : 0.0f;
-        c.bias[e] = there && a.bias ? to_f32<DT>(a.bias[at]) : 0.0f;
+        c.scale[e] = there ? a.b_scales[n + e] : 0.0f;
+        c.bias[e] = there && a.bias ? to_f32<DT>(a.bias[n + e]) : 0.0f;
     }
     return c;
 }
+
+// Four results of a row, in 16 bits.
 template <int DT>
-__device__ __forceinline__ u32x2_t finish(i32x4_t sum, float scale, const Columns& c) {
+__device__ __forceinline__ u32x2_t finish(i32x4_t sum, float row, f32x4_t scale, f32x4_t bias) {
     float v[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (float)sum[e] * scale * c.scale[e] + c.bias[e];
+    for (int e = 0; e < 4; ++e) v[e] = (float)sum[e] * row * scale[e] + bias[e];
     return u32x2_t{pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
 }
 

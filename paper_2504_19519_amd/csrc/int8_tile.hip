@@ -185,10 +185,7 @@ __device__ __forceinline__ void tile_body(const Int8Args& a, const Block& b, con
         static_for<MI>([&](auto ic) __attribute__((always_inline)) {
             constexpr int i = decltype(ic)::value;
             const float row = s.row[row_w + i * 16 + lr];
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = (float)acc[i][j][e] * row * scale[e] + bias[e];
-            const u32x2_t w = {pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
+            const u32x2_t w = finish<DT>(acc[i][j], row, scale, bias);
             const int r = i * 16 + lr, c = col_w / 8 + 2 * j + lq;
             *reinterpret_cast<u32x2_t*>(sb + r * 512 + ((c ^ (r & 31)) << 4) + 8 * lh) = w;
         });
