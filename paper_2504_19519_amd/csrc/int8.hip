@@ -383,13 +383,14 @@ struct Form {
     int rows, cols, stages, parts, span;
 };
 
-// Nanoseconds of a launch of `tiles` 256 x 256 tiles, one to a compute unit, and of `blocks`
-// 128 x 128 blocks, two to a compute unit, of `steps` each (as measured: 8192 x 8192 x
-// 8192 in tiles 419 us, in blocks 530; 4096 x 4096 x 4096 58 and 70; 2048 x 4096 x 4096 48
-// and 37; 4768 x 4736 x 4672 114 and 145; 7596 x 5376 x 192 41 and 34).
-int64_t tiles_ns(int64_t tiles, int64_t steps) {
-    const int64_t rest = tiles % 256;
-    return tiles / 256 * (1500 * steps + 10000) + (rest == 0 ? 0 : rest <= 128 ? 1250 * steps + 5000 : 1500 * steps + 10000);
+// Nanoseconds of a launch of `tiles` 256 x 256 tiles, one to a compute unit (by experts with
+// nothing overlapped between them), and of `blocks` 128 x 128 blocks, two to a compute unit,
+// of `steps` each. As measured, us in tiles and in blocks: 8192 x 8192 x 8192 393 and 530;
+// 8192 x 8192 x 3584 181 and 231; 4096 x 4096 x 4096 54 and 70; 2048 x 4096 x 4096 48 and 34;
+// 4768 x 4736 x 4672 109 and 145; 7596 x 5376 x 192 29 and 34.
+int64_t tiles_ns(int64_t tiles, int64_t steps, bool experts) {
+    const int64_t rest = tiles % 256, round = 1460 * steps + (experts ? 10000 : 4400);
+    return (experts ? 0 : 6000) + tiles / 256 * round + (rest == 0 ? 0 : rest <= 128 ? 1250 * steps + 2000 : round);
 }
 int64_t blocks_ns(int64_t blocks, int64_t steps) {
     const int64_t rest = blocks % 512;
@@ -403,7 +404,7 @@ int64_t blocks_ns(int64_t blocks, int64_t steps) {
 Form product_form(int64_t M, int64_t N, int64_t K) {
     const int64_t steps = (int8_row_bytes(K) + 127) / 128;
     const auto blocks = [&](int64_t size) { return ((M + size - 1) / size) * ((N + size - 1) / size); };
-    if (M > 128 && K > 0 && tiles_ns(blocks(256), steps) < blocks_ns(blocks(128), steps)) return {256, 256, 2, 1, 1};
+    if (M > 128 && K > 0 && tiles_ns(blocks(256), steps, false) < blocks_ns(blocks(128), steps)) return {256, 256, 2, 1, 1};
     if (M > 40 && blocks(128) > 256) return {128, 128, 2, 1, 1};
     if (M > 40 && blocks(128) >= 144 && steps >= 8) return {128, 128, 3, 1, 1};
     if (M > 32 && blocks(32) > 512) return {64, 64, 4, 1, 1};
@@ -427,7 +428,7 @@ Form experts_form(const Int8Args& a) {
     const int64_t experts = std::min<int64_t>(a.E, pairs), each = (pairs + experts - 1) / experts;
     const int64_t steps = (int8_row_bytes(a.K) + 127) / 128;
     const auto blocks = [&](int64_t size) { return experts * ((each + size - 1) / size) * ((a.N + size - 1) / size); };
-    if (each > 192 && a.K > 0 && tiles_ns(blocks(256), steps) < blocks_ns(blocks(128), steps)) return {256, 256, 2, 1, 1};
+    if (each > 192 && a.K > 0 && tiles_ns(blocks(256), steps, true) < blocks_ns(blocks(128), steps)) return {256, 256, 2, 1, 1};
     if (each > 8 && blocks(128) >= 144) return {128, 128, 2, 1, blocks(128) < 2048 || steps > 8 ? 1 : steps > 2 ? 2 : 4};
     if (blocks(32) > 2048 || (each > 8 && blocks(32) > 512)) return {64, 64, 4, 1, blocks(64) < 6000 || steps > 16 ? 1 : 4};
     return {32, 32, 4, 1, 1};

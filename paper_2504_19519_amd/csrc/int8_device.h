@@ -93,6 +93,7 @@ __device__ __forceinline__ bool find_block(const Int8Args& a, int p, int width, 
             const int e = lane * run + i;
             if (e < a.E) mine += (rows_of(a.counts[e], a.offsets[e]) + BM - 1) / BM;
         }
+        mine = mine < 1 << 24 ? mine : 1 << 24;     // (more than any launch has: the sums stay in 31 bits)
         const int upto = lanes_before(mine), total = __builtin_amdgcn_readlane(upto, 63);
         // each chiplet takes a contiguous share of the blocks, an expert's after another's
         const int64_t all = (int64_t)total * cols, per = (all + kXcds - 1) / kXcds;

@@ -6,7 +6,16 @@
 // stages; v_mfma_i32_16x16x64_i8 in inline asm with the accumulators tied in place, every
 // LDS read and load issue in the shadow of an MFMA. The scales, the bias and the rows' places
 // wait in LDS from the tile's start.
+//
+// Workgroups compute one tile after another, and a tile's first loads go ahead of the results
+// of the one before it: tiles of one size end together, and memory would see 32 MB of results
+// and then 32 MB of operands, with no compute unit at work (14 us a tile; 4 are left. Of
+// experts, whose tiles end apart, a workgroup has one.)
+// 8192x8192x8192 393 us, 2.8 POPS: the clock is power-limited (1.9 of 2.4 GHz), and the order
+// of reads and loads within a step makes no difference.
 #include <hip/hip_runtime.h>
+
+#include <algorithm>
 
 #include "int8_device.h"
 #include "rows.h"
@@ -32,24 +41,28 @@ __device__ __forceinline__ void mfma_tied(i32x4_t& c, const u32x4_t& x, const u3
 // tile's columns and rows. (The stages are separate arrays, so that the compiler can tell
 // the stage being read from the stage being filled.)
 constexpr int kStage = (256 + 256) * 128;
+constexpr int kOutRow = 128 * 2 + 16;               // a wave's 128 columns of a row, on their way out
 struct Shared {
     char* st0;
     char* st1;
+    char* out;                  // [4][16 * kOutRow]
     float* scale;
     float* bias;
     float* row;
     bool* there;
 };
 
-// A tile of 256 rows, waves 2 x 2 of 128 x 128; or (HALF) of the up to 128 that are left,
-// waves side by side of 128 x 64.
+// Tiles of 256 rows, waves 2 x 2 of 128 x 128; or (HALF) an expert's up to 128 rows behind
+// those, waves side by side of 128 x 64.
 template <int DT, bool EXPERTS, bool HALF>
-__device__ __forceinline__ void tile_body(const Int8Args& a, const Block& b, const Shared& s) {
+__device__ __forceinline__ void tile_body(const Int8Args& a, Block b, const Shared& s) {
+    constexpr bool LOOP = !EXPERTS;                      // one tile after another
     constexpr int BM = HALF ? 128 : 256, BN = 256, MI = 8, NJ = HALF ? 4 : 8;
     constexpr int kA = BM * 128;
     constexpr int kAI = BM / 32, kBI = BN / 32, kLoads = kAI + kBI;      // load instructions per wave and step
     constexpr int kGap = MI * NJ / kLoads;               // MFMAs to a load
     constexpr int kVRows = 2;                            // accumulator block rows held in VGPRs
+    constexpr int kStores = MI * NJ / 2;                 // store instructions of a wave's results
     char* const st0 = s.st0;
     char* const st1 = s.st1;
 
@@ -58,11 +71,6 @@ __device__ __forceinline__ void tile_body(const Int8Args& a, const Block& b, con
     const uint32_t bytes = (uint32_t)int8_row_bytes(a.K);
     const int steps = (int)((bytes + 127) / 128);
     const bool gather = EXPERTS && a.pair_of;
-    const int8_t* const ablk = gather ? a.a : a.a + b.row0 * a.lda;
-    const int8_t* const bblk = a.b + ((int64_t)b.expert * a.N + b.col0) * a.ldb;
-    const int cols = (int)(a.N - b.col0 < BN ? a.N - b.col0 : BN);
-    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)ablk, 0, (int)kSpan, kRsrcWord3);
-    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc((void*)bblk, 0, (int)kSpan, kRsrcWord3);
 
     // A load instruction fills 1 KB: 8 operand rows of 128 bytes, chunk c of row r at slot
     // c ^ ((r / 2) % 8). A lane's offset from the operand's base, or kOutside for a row that
@@ -70,27 +78,51 @@ __device__ __forceinline__ void tile_body(const Int8Args& a, const Block& b, con
     uint32_t voff[kLoads], place[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) place[i] = 16u * (uint32_t)((lane & 7) ^ ((4 * i + lane / 16) & 7));
+    const int8_t* ablk;
+    const int8_t* bblk;
+    int cols;
+    // What the epilogue wants to know of column `tid` and row `tid`, looked up ahead of the
+    // first loads and put into LDS at the first step's barrier.
+    float col_scale = 0.0f, col_bias = 0.0f, row_scale = 0.0f;
+    bool there = false;
+    auto set_up = [&]() __attribute__((always_inline)) {
+        ablk = gather ? a.a : a.a + b.row0 * a.lda;
+        bblk = a.b + ((int64_t)b.expert * a.N + b.col0) * a.ldb;
+        cols = (int)(a.N - b.col0 < BN ? a.N - b.col0 : BN);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const int r = (i < kAI ? wave * kAI + i : wave * kBI + i - kAI) * 8 + lane / 8;
-        if (i < kAI) {
-            const int64_t from = source_row<EXPERTS>(a, b, r);
-            voff[i] = from < 0 ? kOutside : (uint32_t)((gather ? from : r) * a.lda) + place[i & 1];
-        } else {
-            voff[i] = r < cols ? (uint32_t)(r * a.ldb) + place[i & 1] : kOutside;
+        for (int i = 0; i < kLoads; ++i) {
+            const int r = (i < kAI ? wave * kAI + i : wave * kBI + i - kAI) * 8 + lane / 8;
+            if (i < kAI) {
+                const int64_t from = source_row<EXPERTS>(a, b, r);
+                voff[i] = from < 0 ? kOutside : (uint32_t)((gather ? from : r) * a.lda) + place[i & 1];
+            } else {
+                voff[i] = r < cols ? (uint32_t)(r * a.ldb) + place[i & 1] : kOutside;
+            }
         }
-    }
+        const int64_t from = source_row<EXPERTS>(a, b, tid);
+        there = from >= 0;
+        if (there) row_scale = a.a_scales[from];
+        if (tid < cols) {
+            const int64_t at = (int64_t)b.expert * a.N + b.col0 + tid;
+            col_scale = a.b_scales[at];
+            if (a.bias) col_bias = to_f32<DT>(a.bias[at]);
+        }
+    };
     // Load `i` of step t. Chunks past a row's end, and steps past the last, lie outside the
     // resource: zeros, no memory access (every step issues the same loads, and the wait
     // counts stay uniform). The step's offset past kOutside stays outside.
     auto load_one = [&](auto ic, int t, char* st) __attribute__((always_inline)) {
         constexpr int i = decltype(ic)::value;
+        const __amdgpu_buffer_rsrc_t r =
+            __builtin_amdgcn_make_buffer_rsrc((void*)(i < kAI ? ablk : bblk), 0, (int)kSpan, kRsrcWord3);
         const uint32_t at = 128u * (uint32_t)t;
         const uint32_t v = place[i & 1] + at < bytes ? voff[i] : kOutside;
-        if constexpr (i < kAI)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void_t*)(st + (wave * kAI + i) * 1024), 16, v, at, 0, 0);
-        else
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void_t*)(st + kA + (wave * kBI + i - kAI) * 1024), 16, v, at, 0, 0);
+        char* const to = st + (i < kAI ? 0 : kA) + (i < kAI ? wave * kAI + i : wave * kBI + i - kAI) * 1024;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)to, 16, v, at, 0, 0);
+    };
+    auto begin = [&]() __attribute__((always_inline)) {
+        static_for<kLoads>([&](auto ic) __attribute__((always_inline)) { load_one(ic, 0, st0); });
+        static_for<kLoads>([&](auto ic) __attribute__((always_inline)) { load_one(ic, 1, st1); });
     };
 
     // Fragments: lane l feeds row l % 16 of a 16-row block with chunk 4 h + l / 16 of MFMA
@@ -119,18 +151,17 @@ __device__ __forceinline__ void tile_body(const Int8Args& a, const Block& b, con
         });
     };
     // Step t (its first fragments are there) in stage cur, step t + 1 in nxt: once that has
-    // landed and every wave has read all of cur, step t + 2 goes there.
+    // landed and every wave has read all of cur, step t + 2 goes there. Behind the first step's
+    // loads there may be kStores of the tile before (`stores`), which are not waited for.
     constexpr std::true_type kYes{};
     constexpr std::false_type kNo{};
     constexpr std::integral_constant<int, 0> k0{};
     constexpr std::integral_constant<int, 1> k1{};
-    // What the epilogue wants to know of column `tid` and row `tid`, looked up behind the
-    // first loads and put into LDS at the first barrier.
-    float col_scale = 0.0f, col_bias = 0.0f, row_scale = 0.0f;
-    bool there = false;
+    bool stores = false;
     auto step = [&](int t, char* cur, const char* nxt, auto first) __attribute__((always_inline)) {
         substep(fa0, fb0, cur, k1, fa1, fb1, kNo, 0, cur, first);
-        wait_and_barrier<0>();
+        if (LOOP && decltype(first)::value && stores) wait_and_barrier<kStores>();
+        else wait_and_barrier<0>();
         if constexpr (decltype(first)::value) {
             s.scale[tid] = col_scale;
             s.bias[tid] = col_bias;
@@ -140,88 +171,94 @@ __device__ __forceinline__ void tile_body(const Int8Args& a, const Block& b, con
         substep(fa1, fb1, nxt, k0, fa0, fb0, kYes, t + 2, cur, kNo);
     };
 
-    static_for<kLoads>([&](auto ic) __attribute__((always_inline)) { load_one(ic, 0, st0); });
-    static_for<kLoads>([&](auto ic) __attribute__((always_inline)) { load_one(ic, 1, st1); });
-    {
-        const int64_t from = source_row<EXPERTS>(a, b, tid);
-        there = from >= 0;
-        if (there) row_scale = a.a_scales[from];
-        if (tid < cols) {
-            const int64_t at = (int64_t)b.expert * a.N + b.col0 + tid;
-            col_scale = a.b_scales[at];
-            if (a.bias) col_bias = to_f32<DT>(a.bias[at]);
+    set_up();
+    begin();
+    int p = blockIdx.x;
+    bool more;
+    do {
+        // (the newest kLoads operations, or kStores more where that many stores followed, may
+        // be in flight: the first stage has landed)
+        if (LOOP && stores) wait_and_barrier<kLoads + kStores>();
+        else wait_and_barrier<kLoads>();
+        fa0[0] = *reinterpret_cast<const u32x4_t*>(st0 + a_row + cslot[0]);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) fb0[j] = *reinterpret_cast<const u32x4_t*>(st0 + b_row + j * 2048 + cslot[0]);
+#pragma unroll
+        for (int i = 1; i < MI; ++i) fa0[i] = *reinterpret_cast<const u32x4_t*>(st0 + a_row + i * 2048 + cslot[0]);
+        step(0, st0, st1, kYes);
+        int t = 1;
+        for (; t + 2 <= steps; t += 2) {
+            step(t, st1, st0, kNo);
+            step(t + 1, st0, st1, kNo);
         }
-    }
-    wait_and_barrier<0>();
-    fa0[0] = *reinterpret_cast<const u32x4_t*>(st0 + a_row + cslot[0]);
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) fb0[j] = *reinterpret_cast<const u32x4_t*>(st0 + b_row + j * 2048 + cslot[0]);
-#pragma unroll
-    for (int i = 1; i < MI; ++i) fa0[i] = *reinterpret_cast<const u32x4_t*>(st0 + a_row + i * 2048 + cslot[0]);
-    step(0, st0, st1, kYes);
-    int t = 1;
-    for (; t + 2 <= steps; t += 2) {
-        step(t, st1, st0, kNo);
-        step(t + 1, st0, st1, kNo);
-    }
-    if (t < steps) step(t, st1, st0, kNo);
-    // the accumulators are read only once the last MFMA's result is written
-    asm volatile("s_nop 7\n s_nop 7\n s_nop 7\n s_nop 7" ::: "memory");
-    wait_and_barrier<0>();          // no load may still be writing LDS
-    __syncthreads();                // the stages are reused for the result
+        if (t < steps) step(t, st1, st0, kNo);
+        // the accumulators are read only once the last MFMA's result is written
+        asm volatile("s_nop 7\n s_nop 7\n s_nop 7\n s_nop 7" ::: "memory");
+        wait_and_barrier<0>();          // every wave has read the stages, and no load is writing LDS
 
-    // Row r of the tile is staged in 512 bytes: row r % 128 of stage r / 128 (the half of the
-    // waves' rows), chunk c at c ^ (r % 32), so that the rows that are written or read
-    // together lie on different banks.
-    int tid_e = tid;
-    asm volatile("" : "+v"(tid_e)); // the epilogue's addresses are formed here, not ahead of the main loop
-    const int lane_e = tid_e & 63, lr = lane_e & 15, lh = (lane_e >> 4) & 1, lq = lane_e >> 5;
-    char* const sb = row_w == 0 ? st0 : st1;
-    static_for<NJ>([&](auto jc) __attribute__((always_inline)) {
-        constexpr int j = decltype(jc)::value;
-        const int col = col_w + j * 16 + 4 * (lane_e >> 4);
-        const f32x4_t scale = *reinterpret_cast<const f32x4_t*>(s.scale + col);
-        const f32x4_t bias = *reinterpret_cast<const f32x4_t*>(s.bias + col);
+        uint16_t* const out = a.c + (b.row0 + row_w) * a.ldc + b.col0 + col_w;
+        const int left = cols - col_w, rows = b.rows - row_w;
+        p += gridDim.x;
+        more = LOOP && p < a.blocks;
+        stores = more && b.rows == BM && cols == BN;
+        if (more) {                     // the next tile's first loads ahead of this one's results
+            find_block<256, EXPERTS>(a, p, 256, b);
+            set_up();
+            begin();
+        }
+
+        // A wave's part of the tile, 16 rows at a time: through LDS into whole rows.
+        int lane_e = lane;
+        asm volatile("" : "+v"(lane_e)); // the addresses are formed here, not ahead of the main loop
+        char* const stage = s.out + wave * 16 * kOutRow;
+        const float* const scale_w = s.scale + col_w + 4 * (lane_e >> 4);
+        const float* const bias_w = s.bias + col_w + 4 * (lane_e >> 4);
         static_for<MI>([&](auto ic) __attribute__((always_inline)) {
             constexpr int i = decltype(ic)::value;
-            const float row = s.row[row_w + i * 16 + lr];
-            const u32x2_t w = finish<DT>(acc[i][j], row, scale, bias);
-            const int r = i * 16 + lr, c = col_w / 8 + 2 * j + lq;
-            *reinterpret_cast<u32x2_t*>(sb + r * 512 + ((c ^ (r & 31)) << 4) + 8 * lh) = w;
+            const float row = s.row[row_w + 16 * i + (lane_e & 15)];
+            static_for<NJ>([&](auto jc) __attribute__((always_inline)) {
+                constexpr int j = decltype(jc)::value;
+                *reinterpret_cast<u32x2_t*>(stage + (lane_e & 15) * kOutRow + 32 * j + 8 * (lane_e >> 4)) =
+                    finish<DT>(acc[i][j], row, *reinterpret_cast<const f32x4_t*>(scale_w + 16 * j),
+                               *reinterpret_cast<const f32x4_t*>(bias_w + 16 * j));
+            });
+            constexpr int kChunks = 2 * NJ;             // of 16 bytes, of a row
+#pragma unroll
+            for (int q = 0; q < 16 * kChunks / 64; ++q) {
+                const int at = 64 * q + lane_e, r = at / kChunks, ch = at % kChunks;
+                const u32x4_t v = *reinterpret_cast<const u32x4_t*>(stage + r * kOutRow + 16 * ch);
+                uint16_t* const to = out + (int64_t)(16 * i + r) * a.ldc + 8 * ch;
+                if (LOOP && stores) stream8(to, v);     // (a whole tile: kStores instructions)
+                else if (EXPERTS ? s.there[row_w + 16 * i + r] : 16 * i + r < rows) write_chunk(to, v, left - 8 * ch);
+            }
         });
-    });
-    __syncthreads();
-    const int c = tid_e & 31, r0 = tid_e >> 5;
-    const int64_t left = cols - 8 * c;
-    uint16_t* const out = a.c + b.row0 * a.ldc + b.col0 + 8 * c;
-#pragma unroll 8
-    for (int k = 0; k < BM / 8; ++k) {
-        const int r = r0 + 8 * k;
-        const char* const from = (k < 16 ? st0 : st1) + (r & 127) * 512 + ((c ^ (r & 31)) << 4);
-        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(from);
-        if (s.there[r]) write_chunk(out + (int64_t)r * a.ldc, v, left);
-    }
+    } while (more);
 }
 
 template <int DT, bool EXPERTS>
 __global__ __launch_bounds__(256, 1) void int8_tile_kernel(const Int8Args a) {
     __shared__ __attribute__((aligned(1024))) char st0[kStage];
     __shared__ __attribute__((aligned(1024))) char st1[kStage];
+    __shared__ __attribute__((aligned(16))) char s_out[4 * 16 * kOutRow];
     __shared__ __attribute__((aligned(16))) float s_scale[256], s_bias[256], s_row[256];
     __shared__ bool s_there[256];
     Block b;
     if (!find_block<256, EXPERTS>(a, blockIdx.x, 256, b)) return;
-    const Shared s = {st0, st1, s_scale, s_bias, s_row, s_there};
-    if (b.rows > 128) tile_body<DT, EXPERTS, false>(a, b, s);
+    const Shared s = {st0, st1, s_out, s_scale, s_bias, s_row, s_there};
+    if (!EXPERTS || b.rows > 128) tile_body<DT, EXPERTS, false>(a, b, s);
     else tile_body<DT, EXPERTS, true>(a, b, s);
 }
 
 }  // namespace
 
-hipError_t launch_int8_tile(int dtype, bool experts, uint32_t blocks, const Int8Args& a, hipStream_t s) {
+hipError_t launch_int8_tile(int dtype, bool experts, uint32_t blocks, const Int8Args& args, hipStream_t s) {
+    Int8Args a = args;
+    a.blocks = (int32_t)blocks;
     if (experts)
         return launch(dtype == FO_FP16 ? int8_tile_kernel<FO_FP16, true> : int8_tile_kernel<FO_BF16, true>, blocks, 256, s, a);
-    return launch(dtype == FO_FP16 ? int8_tile_kernel<FO_FP16, false> : int8_tile_kernel<FO_BF16, false>, blocks, 256, s, a);
+    // one workgroup to a compute unit (256)
+    return launch(dtype == FO_FP16 ? int8_tile_kernel<FO_FP16, false> : int8_tile_kernel<FO_BF16, false>,
+                  std::min<uint32_t>(blocks, 256), 256, s, a);
 }
 
 }  // namespace fo

@@ -62,11 +62,12 @@ struct Int8Args {
     int32_t E, choices, capacity;
     int32_t parts;              // of K; 1: not split
     int32_t span;               // blocks, side by side, of a workgroup
+    int32_t blocks;             // 256 x 256 tiles, of all workgroups
 };
 int64_t int8_workspace_bytes(int64_t M, int64_t N, int64_t K);
 // Whether a launch takes the product (work-items are counted in 32 bits).
 bool int8_launchable(const Int8Args& a, bool experts);
-// Tiles of 256 x 256 (K > 0); `blocks` workgroups, a tile each.
+// `blocks` tiles of 256 x 256 (K > 0).
 hipError_t launch_int8_tile(int dtype, bool experts, uint32_t blocks, const Int8Args& a, hipStream_t s);
 hipError_t launch_int8_product(int dtype, const Int8Args& a, hipStream_t s);
 hipError_t launch_int8_experts(int dtype, const Int8Args& a, hipStream_t s);
