@@ -81,9 +81,12 @@ struct RowChunks {
         : n((int)N), last(((int)N - 1) >> 3), twice(SMALL ? 0 : 8 * (last + 1) - (int)N) {}
     // (unsigned, so that an access takes a row's address from scalar registers)
     __device__ __forceinline__ uint32_t column(int c) const { return (uint32_t)(8 * c - (c == last ? twice : 0)); }
+    template <bool STREAMED = false>
     __device__ __forceinline__ u32x4_t read(const uint16_t* row, int c) const {
         if (c > last) return u32x4_t{0u, 0u, 0u, 0u};
-        return SMALL ? read_chunk<kCached>(row, n) : load8(row + column(c));
+        if constexpr (SMALL) return read_chunk<kCached>(row, n);
+        else if constexpr (STREAMED) return stream_load8(row + column(c));
+        else return load8(row + column(c));
     }
     __device__ __forceinline__ void write(uint16_t* row, int c, u32x4_t v) const {
         if (c > last) return;
@@ -187,7 +190,7 @@ constexpr int group_rows(int threads) { return threads < 64 ? 64 / threads : 1; 
 // TH threads to a row, CH chunks each, a wave on several rows where they are short. The
 // next row's loads are issued ahead of this row's sums. NORM: the sum's norm; else the
 // codes of x.
-template <int DT, int CH, int TH, bool NORM, bool SMALL>
+template <int DT, int CH, int TH, bool NORM, bool SMALL, bool STREAMED>
 __global__ __launch_bounds__(TH < 64 ? 64 : TH, 4) void rows8_kernel(const Rows8Args a) {
     constexpr int ROWS = group_rows(TH), kRowWaves = TH / 64;
     __shared__ float s_join[2][2][kRowWaves > 1 ? kRowWaves : 1];
@@ -211,9 +214,9 @@ __global__ __launch_bounds__(TH < 64 ? 64 : TH, 4) void rows8_kernel(const Rows8
 #pragma unroll
         for (int t = 0; t < CH; ++t) {
             const int c = i < a.M ? lane + TH * t : k.last + 1;
-            next[t] = k.read(a.x + i * a.ldx, c);
+            next[t] = k.template read<STREAMED>(a.x + i * a.ldx, c);
             if constexpr (NORM) {
-                if (a.residual) next_r[t] = k.read(a.residual + i * a.ldr, c);
+                if (a.residual) next_r[t] = k.template read<STREAMED>(a.residual + i * a.ldr, c);
             }
         }
     };
@@ -342,7 +345,7 @@ struct GradPart {
 
 // ROWS rows at a time, TH threads each; every thread keeps its columns' sums of
 // dy h r over all of its rows, and the next AHEAD rows' loads are in flight.
-template <int DT, int CH, int TH, int ROWS, int AHEAD, bool SMALL>
+template <int DT, int CH, int TH, int ROWS, int AHEAD, bool SMALL, bool STREAMED>
 __global__ __launch_bounds__(TH * ROWS) void norm_add_backward_kernel(const NormAddArgs a) {
     constexpr int kWaves = TH * ROWS / 64, kRowWaves = TH / 64;
     __shared__ float s_sum[2][kWaves];
@@ -367,10 +370,10 @@ __global__ __launch_bounds__(TH * ROWS) void norm_add_backward_kernel(const Norm
 #pragma unroll
         for (int t = 0; t < CH; ++t) {
             const int c = i < a.M ? lane + TH * t : k.last + 1;
-            p.g[t] = k.read(a.dy + i * a.lddy, c);
-            p.h[t] = k.read(a.h + i * a.ldh, c);
+            p.g[t] = k.template read<STREAMED>(a.dy + i * a.lddy, c);
+            p.h[t] = k.template read<STREAMED>(a.h + i * a.ldh, c);
             p.d[t] = u32x4_t{0u, 0u, 0u, 0u};
-            if (a.dh && a.dx) p.d[t] = k.read(a.dh + i * a.lddh, c);
+            if (a.dh && a.dx) p.d[t] = k.template read<STREAMED>(a.dh + i * a.lddh, c);
         }
         p.rstd = i < a.M ? a.rstd[i] : 0.0f;
     };
@@ -544,7 +547,7 @@ template <int N>
 using Int = std::integral_constant<int, N>;
 
 // A kernel's threads per row and chunks per thread, as go(threads, chunks).
-template <typename F>
+template <bool NORM, typename F>
 hipError_t for_form(int64_t N, F go) {
     if (N <= 64) return go(Int<8>(), Int<1>());
     if (N <= 128) return go(Int<8>(), Int<2>());
@@ -556,7 +559,7 @@ hipError_t for_form(int64_t N, F go) {
     if (N <= 6144) return go(Int<256>(), Int<3>());
     if (N <= 8192) return go(Int<512>(), Int<2>());
     if (N <= 12288) return go(Int<512>(), Int<3>());
-    if (N <= 16384) return go(Int<512>(), Int<4>());
+    if (N <= 16384) return NORM ? go(Int<512>(), Int<4>()) : go(Int<1024>(), Int<2>());
     if (N <= 24576) return go(Int<1024>(), Int<3>());
     return go(Int<1024>(), Int<4>());
 }
@@ -587,9 +590,15 @@ hipError_t for_backward(const NormForm& f, F go) {
 
 }  // namespace
 
+// Whether a call's matrices are too large for the caches to keep any of them until they are
+// read again; their loads then leave the caches to what is written (nontemporal). us, loads
+// kept and not: norm_add and its backward pass 1217x2880 17.7 and 18.9, 8192x1024 27.6 and
+// 31.1, 4096x4096 54.4 and 52.7, 16384x4096 188 and 180; quantize 16384x4096 41.7 and 36.5.
+static bool streams(int64_t M, int64_t N) { return M * N > (int64_t)1 << 24; }
+
 template <bool NORM>
 static hipError_t launch_rows8(int dtype, const Rows8Args& a, hipStream_t s) {
-    return for_form(a.N, [&](auto th, auto ch) {
+    return for_form<NORM>(a.N, [&](auto th, auto ch) {
         constexpr int TH = decltype(th)::value, CH = decltype(ch)::value, kThreads = TH < 64 ? 64 : TH;
         // Waves over all compute units (256): the more of a row they have in flight each, the
         // fewer. (us: 8192x8192 bf16 to codes with 2048, 4096 and 8192 waves 66, 44, 41; its
@@ -598,13 +607,15 @@ static hipError_t launch_rows8(int dtype, const Rows8Args& a, hipStream_t s) {
         const int64_t rows = group_rows(TH), groups = (a.M + rows - 1) / rows;
         const int64_t waves = !NORM ? 8192 : groups * kThreads / 64 >= 16 * 2048 ? 2048 : 4096;
         const uint32_t blocks = (uint32_t)std::min<int64_t>(groups, waves * 64 / kThreads);
+        auto go = [&](auto small, auto streamed) {
+            constexpr bool SMALL = decltype(small)::value, STREAMED = decltype(streamed)::value;
+            return launch(dtype == FO_FP16 ? rows8_kernel<FO_FP16, CH, TH, NORM, SMALL, STREAMED>
+                                           : rows8_kernel<FO_BF16, CH, TH, NORM, SMALL, STREAMED>, blocks, kThreads, s, a);
+        };
         if constexpr (TH == 8 && CH == 1) {
-            if (a.N < 8)
-                return launch(dtype == FO_FP16 ? rows8_kernel<FO_FP16, CH, TH, NORM, true> : rows8_kernel<FO_BF16, CH, TH, NORM, true>,
-                              blocks, kThreads, s, a);
+            if (a.N < 8) return go(std::true_type(), std::false_type());
         }
-        return launch(dtype == FO_FP16 ? rows8_kernel<FO_FP16, CH, TH, NORM, false> : rows8_kernel<FO_BF16, CH, TH, NORM, false>,
-                      blocks, kThreads, s, a);
+        return streams(a.M, a.N) ? go(std::false_type(), std::true_type()) : go(std::false_type(), std::false_type());
     });
 }
 
@@ -634,15 +645,19 @@ hipError_t launch_norm_add_backward(int dtype, const NormAddArgs& a, float* dgam
             constexpr int CH = decltype(ch)::value, TH = decltype(th)::value, ROWS = decltype(rows)::value;
             constexpr int AHEAD = 1;
             blocks = std::min<int64_t>((a.M + ROWS - 1) / ROWS, 256);
+            auto go = [&](auto small, auto streamed) {
+                constexpr bool SMALL = decltype(small)::value, STREAMED = decltype(streamed)::value;
+                return launch(dtype == FO_FP16 ? norm_add_backward_kernel<FO_FP16, CH, TH, ROWS, AHEAD, SMALL, STREAMED>
+                                               : norm_add_backward_kernel<FO_BF16, CH, TH, ROWS, AHEAD, SMALL, STREAMED>,
+                              (uint32_t)blocks, TH * ROWS, s, a);
+            };
             if constexpr (TH == 8) {
-                if (a.N < 8)
-                    return launch(dtype == FO_FP16 ? norm_add_backward_kernel<FO_FP16, CH, TH, ROWS, AHEAD, true>
-                                                   : norm_add_backward_kernel<FO_BF16, CH, TH, ROWS, AHEAD, true>,
-                                  (uint32_t)blocks, TH * ROWS, s, a);
+                if (a.N < 8) return go(std::true_type(), std::false_type());
             }
-            return launch(dtype == FO_FP16 ? norm_add_backward_kernel<FO_FP16, CH, TH, ROWS, AHEAD, false>
-                                           : norm_add_backward_kernel<FO_BF16, CH, TH, ROWS, AHEAD, false>,
-                          (uint32_t)blocks, TH * ROWS, s, a);
+            if constexpr (TH * ROWS >= 768) {       // (as many rows at a time as there are threads for, then)
+                if (streams(a.M, a.N)) return go(std::false_type(), std::true_type());
+            }
+            return go(std::false_type(), std::false_type());
         });
     }
     if (e == hipSuccess && dgamma) e = launch_norm_reduce(a.partial, (int)blocks, a.N, dgamma, nullptr, s);

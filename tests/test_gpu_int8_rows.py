@@ -333,3 +333,38 @@ def test_no_rows_zero_the_sums():
     assert (dgamma == 0).all()
     fo.quantize_rows(None, None, None, 0, 40, "bf16")
     fo.norm_add_forward(None, None, None, None, None, 0, 40, "bf16")
+
+
+@pytest.mark.parametrize("M,N", [(300000, 57), (140000, 121), (70000, 250), (35000, 500), (17000, 1001), (9000, 2000), (4200, 4099),
+                                 (2900, 6000), (2100, 8190), (1500, 12001), (1100, 16000), (700, 24570)])
+def test_matrices_past_the_caches(M, N):
+    """Sizes whose loads pass the caches by: the first, the last and some rows between against
+    the reference, the sums over all rows against 64 bits on the GPU."""
+    torch = torch_mod()
+    assert M * N > 1 << 24
+    dtype = "bf16"
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    x, r, dy, dh = (torch.randn(M, N, generator=gen, device="cuda").bfloat16() for _ in range(4))
+    gamma = (torch.rand(N, generator=gen, device="cuda") + 0.5).bfloat16()
+    at = np.unique(np.concatenate([np.arange(20), np.arange(M - 20, M), np.random.default_rng(M).integers(0, M, 40)]))
+    some = lambda t: t[torch.as_tensor(at).cuda()].double().cpu().numpy()
+    codes, scales = torch.zeros(M, fo.int8_row_bytes(N), dtype=torch.int8, device="cuda"), f32_vec(M)
+    fo.quantize_rows(x, codes, scales, M, N, dtype)
+    check_quantized(some(codes)[:, :N].astype(np.int8), some(scales).astype(np.float32), some(x), "quantize")
+    assert not bool(codes[:, N:].any())
+    h, y, dx = (torch.empty_like(x) for _ in range(3))
+    rstd, dgamma = f32_vec(M), f32_vec(N)
+    fo.norm_add_forward(x, r, gamma, h, y, M, N, dtype, 1e-6, rstd=rstd, codes=codes, scales=scales)
+    want_h = kept_sum(some(x), some(r), dtype)
+    np.testing.assert_array_equal(some(h), want_h)
+    g = host(gamma)
+    want_r, want = ref.norm_add(want_h, g, 1e-6)
+    close(some(rstd), want_r, want_r * RSTD, "rstd")
+    close(some(y), want, rounded(want, dtype, np.abs(want) * (RSTD + 2 * F32)), "y", dtype)
+    check_norm_codes(some(codes)[:, :N].astype(np.int8), some(scales), want_h, g, want_r, "codes")
+    work = torch.empty(fo.norm_workspace_bytes(M, N), dtype=torch.uint8, device="cuda")
+    fo.norm_add_backward(dy, dh, h, gamma, rstd, dx, dgamma, M, N, dtype, work)
+    check_grads(some(dx), None, some(dy), some(dh), want_h, g, some(rstd), dtype, "backward")
+    terms = dy.double() * h.double() * rstd.double()[:, None]
+    steps = -(-M // 64) + 24 + 3
+    close(dgamma.cpu().numpy(), terms.sum(0).cpu().numpy(), steps * F32 * terms.abs().sum(0).cpu().numpy(), "dgamma")
