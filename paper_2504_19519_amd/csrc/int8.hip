@@ -28,8 +28,10 @@ namespace {
 // Four waves, 2 x 2, on a block of BM x BN. k steps of 128, moving from memory straight
 // into an LDS ring of ST stages; the next substep's fragments are read while the MFMAs
 // of the current one run, one barrier per step. An operand row of a step is 128 bytes,
-// chunk c of row r at slot c ^ ((r / 2) % 8): 16 rows' chunks lie on different banks.
-template <int DT, int BM, int BN, int ST, bool EXPERTS>
+// chunk c of row r at slot c ^ ((r / 2) % 8): 16 rows' chunks lie on different banks. ONCE:
+// the weights' loads are past the caches' keeping.
+constexpr int kNontemporal = 2;         // cache policy of a buffer load
+template <int DT, int BM, int BN, int ST, bool EXPERTS, bool ONCE>
 __global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 ? 1 : 2) void int8_block_kernel(const Int8Args a) {
     constexpr int kWaves = 4, WTM = BM / 2, WTN = BN / 2, MI = WTM / 16, NJ = WTN / 16;
     constexpr int kA = BM * 128, kStage = (BM + BN) * 128;
@@ -114,7 +116,8 @@ __global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 ? 1 : 2) void int8_bloc
         const uint32_t at = 128u * (uint32_t)(first + t);
         const uint32_t v = place[i] + at < (uint32_t)bytes ? voff[i] : kOutside;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            r, (lds_void_t*)(st + (is_a ? 0 : kA) + (is_a ? wave * kAI + i : wave * kBI + i - kAI) * 1024), 16, v, at, 0, 0);
+            r, (lds_void_t*)(st + (is_a ? 0 : kA) + (is_a ? wave * kAI + i : wave * kBI + i - kAI) * 1024), 16, v, at, 0,
+            ONCE && !is_a ? kNontemporal : 0);
     };
     // The first loads of the block at b.col0.
     auto begin = [&]() __attribute__((always_inline)) {
@@ -423,8 +426,9 @@ Form product_form(int64_t M, int64_t N, int64_t K) {
 //                          2048 columns   K 7168  1: 201 / 173 / 177  2: 230 / 179 / 183  4: - / 198 / 189
 //   512 tokens to 8 of 64, 2048 columns   K 2048  1: 70 / 79     2: 85 / 77 / 103
 //   1217 tokens to 4 of 60, 2881 columns  K 1409  1: 94 / 116    2: 95 / 115 / 154   (in tiles 110)
+int64_t pairs_of(const Int8Args& a) { return a.pair_of ? std::min<int64_t>(a.capacity, a.a_rows * a.choices) : a.capacity; }
 Form experts_form(const Int8Args& a) {
-    const int64_t pairs = a.pair_of ? std::min<int64_t>(a.capacity, a.a_rows * a.choices) : a.capacity;
+    const int64_t pairs = pairs_of(a);
     const int64_t experts = std::min<int64_t>(a.E, pairs), each = (pairs + experts - 1) / experts;
     const int64_t steps = (int8_row_bytes(a.K) + 127) / 128;
     const auto blocks = [&](int64_t size) { return experts * ((each + size - 1) / size) * ((a.N + size - 1) / size); };
@@ -437,13 +441,30 @@ Form experts_form(const Int8Args& a) {
 template <int N>
 using Int = std::integral_constant<int, N>;
 
+// Whether the weights are read once by the call and too large to be found in the caches by the
+// next one: their loads then leave the caches alone. Rows that do not begin with a line of 128
+// bytes share lines between steps, and need them kept. us, loads kept and not: 16 tokens to 8
+// of 256 experts, 2048 x 7168 171 and 157; 16 x 16384 x 16384 64 and 58; but 16 x 14336 x 4096,
+// which the caches hold, 11.6 and 15.4; 1217 tokens to 4 of 60, rows of 1424 bytes 95 and 117.
+bool weights_once(const Int8Args& a, const Form& f, bool experts) {
+    if (a.ldb % 128 != 0) return false;
+    if (!experts) return a.M <= f.rows && a.N * a.ldb > (int64_t)1 << 27;
+    const int64_t pairs = pairs_of(a), some = std::min<int64_t>(a.E, pairs);
+    return pairs <= f.rows * some && some * a.N * a.ldb > (int64_t)1 << 27;
+}
+
 template <bool EXPERTS>
 hipError_t launch_any(int dtype, const Int8Args& a, const Form& f, hipStream_t s) {
     const dim3 grid((uint32_t)blocks_of<EXPERTS>(a, f.rows, f.cols * f.span), (uint32_t)f.parts);
     const auto block = [&](auto bm, auto bn, auto st) {
         constexpr int BM = decltype(bm)::value, BN = decltype(bn)::value, ST = decltype(st)::value;
-        return launch(dtype == FO_FP16 ? int8_block_kernel<FO_FP16, BM, BN, ST, EXPERTS>
-                                       : int8_block_kernel<FO_BF16, BM, BN, ST, EXPERTS>, grid, 256, s, a);
+        if constexpr (BM <= 64) {
+            if (weights_once(a, f, EXPERTS))
+                return launch(dtype == FO_FP16 ? int8_block_kernel<FO_FP16, BM, BN, ST, EXPERTS, true>
+                                               : int8_block_kernel<FO_BF16, BM, BN, ST, EXPERTS, true>, grid, 256, s, a);
+        }
+        return launch(dtype == FO_FP16 ? int8_block_kernel<FO_FP16, BM, BN, ST, EXPERTS, false>
+                                       : int8_block_kernel<FO_BF16, BM, BN, ST, EXPERTS, false>, grid, 256, s, a);
     };
     if (f.rows == 256) return launch_int8_tile(dtype, EXPERTS, grid.x, a, s);
     if (f.rows == 128) return f.stages == 2 ? block(Int<128>(), Int<128>(), Int<2>()) : block(Int<128>(), Int<128>(), Int<3>());

@@ -97,6 +97,13 @@ def test_inner_sizes_that_are_split(M, N, K, bias):
     check(M, N, K, "fp16", bias=bias, ldc=N + 5)
 
 
+@pytest.mark.parametrize("M", [7, 64])
+def test_weights_past_the_caches(M):
+    """More than 128 MiB of weights, in lines of their own, under few rows; and the same of experts."""
+    check(M, 16500, 8192, "bf16", bias=True)
+    Experts(M, 2, 33, 1000, 4096, "bf16", True, bias=True).check()
+
+
 @pytest.mark.parametrize("M", [3, 20, 50, 90, 400])
 def test_rows_apart(M):
     """Strides of all three matrices, guards between their rows (the codes' are no zeros)."""
