@@ -467,7 +467,10 @@ hipError_t launch_any(int dtype, const Int8Args& a, const Form& f, hipStream_t s
                                        : int8_block_kernel<FO_BF16, BM, BN, ST, EXPERTS, false>, grid, 256, s, a);
     };
     if (f.rows == 256) return launch_int8_tile(dtype, EXPERTS, grid.x, a, s);
-    if (f.rows == 128) return f.stages == 2 ? block(Int<128>(), Int<128>(), Int<2>()) : block(Int<128>(), Int<128>(), Int<3>());
+    if constexpr (!EXPERTS) {
+        if (f.rows == 128 && f.stages == 3) return block(Int<128>(), Int<128>(), Int<3>());
+    }
+    if (f.rows == 128) return block(Int<128>(), Int<128>(), Int<2>());
     if (f.rows == 64) return block(Int<64>(), Int<64>(), Int<4>());
     if constexpr (!EXPERTS) {
         if (f.rows == 16)

@@ -83,17 +83,20 @@ __device__ __forceinline__ void tile_body(const Int8Args& a, Block b, const Shar
     int cols;
     // What the epilogue wants to know of column `tid` and row `tid`, looked up ahead of the
     // first loads and put into LDS at the first step's barrier.
-    float col_scale = 0.0f, col_bias = 0.0f, row_scale = 0.0f;
+    float col_scale = 0.0f, row_scale = 0.0f;
+    uint16_t col_bias = 0;
     bool there = false;
     auto set_up = [&]() __attribute__((always_inline)) {
+        int lane_s = lane;              // formed anew for each tile: kept across it, the offsets go to scratch memory
+        asm volatile("" : "+v"(lane_s));
         ablk = gather ? a.a : a.a + b.row0 * a.lda;
         bblk = a.b + ((int64_t)b.expert * a.N + b.col0) * a.ldb;
         cols = (int)(a.N - b.col0 < BN ? a.N - b.col0 : BN);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int r = (i < kAI ? wave * kAI + i : wave * kBI + i - kAI) * 8 + lane / 8;
+            const int r = (i < kAI ? wave * kAI + i : wave * kBI + i - kAI) * 8 + lane_s / 8;
             if (i < kAI) {
-                const int64_t from = source_row<EXPERTS>(a, b, r);
+                const int64_t from = EXPERTS ? source_row<EXPERTS>(a, b, r) : r < b.rows ? r : -1;
                 voff[i] = from < 0 ? kOutside : (uint32_t)((gather ? from : r) * a.lda) + place[i & 1];
             } else {
                 voff[i] = r < cols ? (uint32_t)(r * a.ldb) + place[i & 1] : kOutside;
@@ -105,7 +108,7 @@ __device__ __forceinline__ void tile_body(const Int8Args& a, Block b, const Shar
         if (tid < cols) {
             const int64_t at = (int64_t)b.expert * a.N + b.col0 + tid;
             col_scale = a.b_scales[at];
-            if (a.bias) col_bias = to_f32<DT>(a.bias[at]);
+            if (a.bias) col_bias = a.bias[at];
         }
     };
     // Load `i` of step t. Chunks past a row's end, and steps past the last, lie outside the
@@ -164,7 +167,7 @@ __device__ __forceinline__ void tile_body(const Int8Args& a, Block b, const Shar
         else wait_and_barrier<0>();
         if constexpr (decltype(first)::value) {
             s.scale[tid] = col_scale;
-            s.bias[tid] = col_bias;
+            s.bias[tid] = to_f32<DT>(col_bias);
             s.row[tid] = row_scale;
             s.there[tid] = there;
         }

@@ -344,8 +344,8 @@ struct GradPart {
 };
 
 // ROWS rows at a time, TH threads each; every thread keeps its columns' sums of
-// dy h r over all of its rows, and the next AHEAD rows' loads are in flight.
-template <int DT, int CH, int TH, int ROWS, int AHEAD, bool SMALL, bool STREAMED>
+// dy h r over all of its rows, and the next row's loads are in flight.
+template <int DT, int CH, int TH, int ROWS, bool SMALL, bool STREAMED>
 __global__ __launch_bounds__(TH * ROWS) void norm_add_backward_kernel(const NormAddArgs a) {
     constexpr int kWaves = TH * ROWS / 64, kRowWaves = TH / 64;
     __shared__ float s_sum[2][kWaves];
@@ -379,11 +379,9 @@ __global__ __launch_bounds__(TH * ROWS) void norm_add_backward_kernel(const Norm
     };
     int64_t i = (int64_t)blockIdx.x * ROWS + group;
     const int64_t rounds = (a.M - (int64_t)blockIdx.x * ROWS + step - 1) / step;   // the same for every row group
-    GradPart<CH> ahead[AHEAD];
-#pragma unroll
-    for (int d = 0; d < AHEAD; ++d) load(i + d * step, ahead[d]);
-    // one round: the row i whose loads `next` holds, which then takes those of row i + AHEAD * step
-    auto round = [&](int64_t n, GradPart<CH>& next) {
+    GradPart<CH> next;
+    load(i, next);
+    for (int64_t n = 0; n < rounds; ++n, i += step) {
         const float rstd = next.rstd;
         float hv[CH][8], gv[CH][8], s = 0.0f;
         u32x4_t dv[CH];
@@ -403,7 +401,7 @@ __global__ __launch_bounds__(TH * ROWS) void norm_add_backward_kernel(const Norm
             }
             s += k.sum(lane + TH * t, [&](int e) { return gv[t][e] * hv[t][e]; });
         }
-        load(i + AHEAD * step, next);
+        load(i + step, next);
         s = lanes_sum<(TH < 64 ? TH : 64)>(s);
         if constexpr (kRowWaves > 1) {
             // (two sets of words, so that one barrier per row is enough)
@@ -423,16 +421,7 @@ __global__ __launch_bounds__(TH * ROWS) void norm_add_backward_kernel(const Norm
                 k.write(a.dx + i * a.lddx, lane + TH * t, narrow<DT>(d));
             }
         }
-        i += step;
-    };
-    int64_t n = 0;
-    for (; n + AHEAD <= rounds; n += AHEAD) {
-#pragma unroll
-        for (int d = 0; d < AHEAD; ++d) round(n + d, ahead[d]);
     }
-#pragma unroll
-    for (int d = 0; d < AHEAD - 1; ++d)
-        if (n + d < rounds) round(n + d, ahead[d]);
 
     if (!a.partial) return;
     // the row groups' sums, the upper half of them added to the lower one until one is left
@@ -572,7 +561,8 @@ hipError_t for_rows(int rows, F go) {
     }
     return go(Int<CH>(), Int<TH>(), Int<MAX>());
 }
-// As norm_backward_form has it.
+// As norm_backward_form has it, or fewer rows at a time (of which every workgroup then has
+// some): half as many kernels.
 template <typename F>
 hipError_t for_backward(const NormForm& f, F go) {
     switch (f.threads) {
@@ -643,12 +633,11 @@ hipError_t launch_norm_add_backward(int dtype, const NormAddArgs& a, float* dgam
     } else if (a.M > 0) {
         e = for_backward(f, [&](auto ch, auto th, auto rows) {
             constexpr int CH = decltype(ch)::value, TH = decltype(th)::value, ROWS = decltype(rows)::value;
-            constexpr int AHEAD = 1;
-            blocks = std::min<int64_t>((a.M + ROWS - 1) / ROWS, 256);
+            blocks = std::min<int64_t>((a.M + ROWS - 1) / ROWS, f.blocks);      // (whose sums the workspace holds)
             auto go = [&](auto small, auto streamed) {
                 constexpr bool SMALL = decltype(small)::value, STREAMED = decltype(streamed)::value;
-                return launch(dtype == FO_FP16 ? norm_add_backward_kernel<FO_FP16, CH, TH, ROWS, AHEAD, SMALL, STREAMED>
-                                               : norm_add_backward_kernel<FO_BF16, CH, TH, ROWS, AHEAD, SMALL, STREAMED>,
+                return launch(dtype == FO_FP16 ? norm_add_backward_kernel<FO_FP16, CH, TH, ROWS, SMALL, STREAMED>
+                                               : norm_add_backward_kernel<FO_BF16, CH, TH, ROWS, SMALL, STREAMED>,
                               (uint32_t)blocks, TH * ROWS, s, a);
             };
             if constexpr (TH == 8) {
