@@ -10,7 +10,11 @@
 // and its output. The codes of y need no r: with t = h gamma, 127 y / max|y| is 127 t /
 // max|t|, and t, a product of two 16-bit values, is exact in fp32. So one meeting of
 // the row's threads gives the sum of squares and the maximum, and the codes are those
-// of exact arithmetic (code_of).
+// of exact arithmetic (codes_of).
+//
+// bf16: 8192x14336 to codes 62 us (5.7 TB/s); the norm of 16384x4096 to 16 bits 86 us and its
+// backward pass 87 (6.3 TB/s), the norm of 8192x4096 to h and codes 41 (6.3). A copy of 1 GiB
+// reaches 6.25 TB/s.
 //
 // Rows end anywhere: the thread with a row's last chunk of eight takes the row's last
 // eight values instead, some of them a second time. It writes what their own thread
