@@ -388,14 +388,13 @@ struct Form {
     int rows, cols, stages, parts, span;
 };
 
-// Nanoseconds of a launch of `tiles` 256 x 256 tiles, one to a compute unit (by experts with
-// nothing overlapped between them), and of `blocks` 128 x 128 blocks, two to a compute unit,
-// of `steps` each. As measured, us in tiles and in blocks: 8192 x 8192 x 8192 393 and 530;
-// 8192 x 8192 x 3584 181 and 231; 4096 x 4096 x 4096 54 and 70; 2048 x 4096 x 4096 48 and 34;
-// 4768 x 4736 x 4672 109 and 145; 7596 x 5376 x 192 29 and 34.
-int64_t tiles_ns(int64_t tiles, int64_t steps, bool experts) {
-    const int64_t rest = tiles % 256, round = 1460 * steps + (experts ? 10000 : 4400);
-    return (experts ? 0 : 6000) + tiles / 256 * round + (rest == 0 ? 0 : rest <= 128 ? 1250 * steps + 2000 : round);
+// Nanoseconds of a launch of `tiles` 256 x 256 tiles, one to a compute unit, and of `blocks`
+// 128 x 128 blocks, two to a compute unit, of `steps` each. As measured, us in tiles and in
+// blocks: 8192 x 8192 x 8192 393 and 530; 8192 x 8192 x 3584 181 and 231; 4096 x 4096 x 4096 54
+// and 70; 2048 x 4096 x 4096 48 and 34; 4768 x 4736 x 4672 109 and 145; 7596 x 5376 x 192 29 and 34.
+int64_t tiles_ns(int64_t tiles, int64_t steps) {
+    const int64_t rest = tiles % 256, round = 1460 * steps + 4400;
+    return 6000 + tiles / 256 * round + (rest == 0 ? 0 : rest <= 128 ? 1250 * steps + 2000 : round);
 }
 int64_t blocks_ns(int64_t blocks, int64_t steps) {
     const int64_t rest = blocks % 512;
@@ -409,7 +408,7 @@ int64_t blocks_ns(int64_t blocks, int64_t steps) {
 Form product_form(int64_t M, int64_t N, int64_t K) {
     const int64_t steps = (int8_row_bytes(K) + 127) / 128;
     const auto blocks = [&](int64_t size) { return ((M + size - 1) / size) * ((N + size - 1) / size); };
-    if (M > 128 && K > 0 && tiles_ns(blocks(256), steps, false) < blocks_ns(blocks(128), steps)) return {256, 256, 2, 1, 1};
+    if (M > 128 && K > 0 && tiles_ns(blocks(256), steps) < blocks_ns(blocks(128), steps)) return {256, 256, 2, 1, 1};
     if (M > 40 && blocks(128) > 256) return {128, 128, 2, 1, 1};
     if (M > 40 && blocks(128) >= 144 && steps >= 8) return {128, 128, 3, 1, 1};
     if (M > 32 && blocks(32) > 512) return {64, 64, 4, 1, 1};
@@ -428,13 +427,24 @@ Form product_form(int64_t M, int64_t N, int64_t K) {
 //                          2048 columns   K 7168  1: 201 / 173 / 177  2: 230 / 179 / 183  4: - / 198 / 189
 //   512 tokens to 8 of 64, 2048 columns   K 2048  1: 70 / 79     2: 85 / 77 / 103
 //   1217 tokens to 4 of 60, 2881 columns  K 1409  1: 94 / 116    2: 95 / 115 / 154   (in tiles 110)
+// Tiles or blocks of 128, for experts of which each has more rows or fewer than the average (of
+// a tile's rows behind the last whole one, half have a half tile): us, bf16, tiles and blocks:
+//   1200 tokens to 8 of 64, 2048 columns  K 7168  280 / 272     1600 tokens  285 / 316
+//   2400 tokens to 8 of 64, 7168 columns  K 2048  389 / 449     4096 tokens, K 512  246 / 307
+//   1000 tokens to 2 of 8,  4096 columns  K 4096   61 /  80     2000 tokens  105 / 106
+//   8192 tokens to 4 of 60, 2881 columns  K 1409  248 / 285     6000 tokens, 300 columns, K 4000  110 / 83
+//   8192 tokens to 1 of 16, 1024 columns  K 1024   23 /  21     1500 to 2 of 16, 1408 columns, K 2048  31 / 19
 int64_t pairs_of(const Int8Args& a) { return a.pair_of ? std::min<int64_t>(a.capacity, a.a_rows * a.choices) : a.capacity; }
 Form experts_form(const Int8Args& a) {
     const int64_t pairs = pairs_of(a);
     const int64_t experts = std::min<int64_t>(a.E, pairs), each = (pairs + experts - 1) / experts;
     const int64_t steps = (int8_row_bytes(a.K) + 127) / 128;
     const auto blocks = [&](int64_t size) { return experts * ((each + size - 1) / size) * ((a.N + size - 1) / size); };
-    if (each > 192 && a.K > 0 && tiles_ns(blocks(256), steps, true) < blocks_ns(blocks(128), steps)) return {256, 256, 2, 1, 1};
+    // (the last round of tiles or blocks half full)
+    const double tiles = (double)((a.N + 255) / 256) * ((double)pairs / 256 + 0.28 * (double)experts) / 256 + 0.5;
+    const double pieces = (double)((a.N + 127) / 128) * ((double)pairs / 128 + 0.5 * (double)experts) / 512 + 0.5;
+    if (each > 160 && a.K > 0 && 6000 + tiles * (double)(1460 * steps + 4400) < pieces * (double)(1030 * steps + 4000))
+        return {256, 256, 2, 1, 1};
     if (each > 8 && blocks(128) >= 144) return {128, 128, 2, 1, blocks(128) < 2048 || steps > 8 ? 1 : steps > 2 ? 2 : 4};
     if (blocks(32) > 2048 || (each > 8 && blocks(32) > 512)) return {64, 64, 4, 1, blocks(64) < 6000 || steps > 16 ? 1 : 4};
     return {32, 32, 4, 1, 1};

@@ -65,57 +65,77 @@ __device__ __forceinline__ int lanes_before(int v) {
     return v;
 }
 
-// The block of workgroup `p` of those of BM rows and `width` columns; false: none. Experts:
-// every wave adds up the experts' blocks.
+// An expert's rows of c: the first, and how many (those below the capacity).
+struct ExpertRows {
+    int first, count;
+};
+__device__ __forceinline__ ExpertRows expert_rows(const Int8Args& a, int e) {
+    const int o = a.offsets[e], n = a.counts[e], most = o < 0 || o > a.capacity ? 0 : a.capacity - o;
+    return {o, n < 0 ? 0 : n > most ? most : n};
+}
+
+// The experts' row blocks of BM: lane l adds up those of experts l run .. l run + run - 1,
+// run = ceil(E / 64). rows_of(e): an expert's rows.
+struct Survey {
+    int mine, upto;             // of the lane's experts, and of all up to them
+};
+template <int BM, typename F>
+__device__ __forceinline__ Survey survey(const Int8Args& a, F rows_of) {
+    const int lane = threadIdx.x & 63, run = (a.E + 63) / 64;
+    Survey s = {0, 0};
+#pragma unroll 4
+    for (int i = 0; i < run; ++i) {
+        const int e = lane * run + i;
+        if (e < a.E) s.mine += (rows_of(e).count + BM - 1) / BM;
+    }
+    s.mine = s.mine < 1 << 24 ? s.mine : 1 << 24;       // (more than any launch has: the sums stay in 31 bits)
+    s.upto = lanes_before(s.mine);
+    return s;
+}
+
+// The block at position `p` of those of BM rows and `width` columns of the experts; false: none.
+template <int BM, typename F>
+__device__ __forceinline__ bool locate(const Int8Args& a, const Survey& s, F rows_of, int p, int width, Block& b) {
+    const int lane = threadIdx.x & 63, run = (a.E + 63) / 64, cols = (int)((a.N + width - 1) / width);
+    // each chiplet takes a contiguous share of the blocks, an expert's after another's
+    constexpr int kXcds = 8;
+    const int64_t all = (int64_t)__builtin_amdgcn_readlane(s.upto, 63) * cols, per = (all + kXcds - 1) / kXcds;
+    const int64_t l = p / kXcds, t = (int64_t)(p % kXcds) * per + l;
+    if (l >= per || t >= all) return false;
+    const int at = (int)(t / cols);             // among the experts' row blocks
+    const int owner = __builtin_ctzll(__builtin_amdgcn_ballot_w64(s.upto > at));
+    const int before = __builtin_amdgcn_readlane(s.upto, owner) - __builtin_amdgcn_readlane(s.mine, owner);
+    // the owner's experts, one to a lane
+    const int e = owner * run + lane;
+    ExpertRows mine = {0, 0};
+    if (lane < run && e < a.E) mine = rows_of(e);
+    const int past = before + lanes_before((mine.count + BM - 1) / BM);
+    const int w = __builtin_ctzll(__builtin_amdgcn_ballot_w64(past > at));
+    const int n = __builtin_amdgcn_readlane(mine.count, w), high = (n + BM - 1) / BM;
+    const int first = __builtin_amdgcn_readlane(past, w) - high;
+    // (an expert's row blocks side by side: they share its weights)
+    const int inside = (int)(t - (int64_t)first * cols), r = inside % high * BM;
+    b.expert = owner * run + w;
+    b.row0 = (int64_t)__builtin_amdgcn_readlane(mine.first, w) + r;
+    b.col0 = (int64_t)(inside / high) * width;
+    b.rows = n - r < BM ? n - r : BM;
+    return true;
+}
+
+// The block of workgroup `p` of those of BM rows and `width` columns; false: none.
 template <int BM, bool EXPERTS>
 __device__ __forceinline__ bool find_block(const Int8Args& a, int p, int width, Block& b) {
-    const int cols = (int)((a.N + width - 1) / width);
-    constexpr int kXcds = 8;
-    if constexpr (!EXPERTS) {
-        const int rows = (int)((a.M + BM - 1) / BM), blocks = rows * cols;
+    if constexpr (EXPERTS) {
+        const auto rows_of = [&](int e) { return expert_rows(a, e); };
+        return locate<BM>(a, survey<BM>(a, rows_of), rows_of, p, width, b);
+    } else {
+        constexpr int kXcds = 8;
+        const int cols = (int)((a.N + width - 1) / width), rows = (int)((a.M + BM - 1) / BM), blocks = rows * cols;
         const int t = tile_of_position(p, rows, cols, FO_ORDER_XCD, rows < 4 ? rows : 4, blocks < kXcds ? blocks : kXcds);
         b.row0 = (int64_t)(t / cols) * BM;
         b.col0 = (int64_t)(t % cols) * width;
         b.rows = (int)(a.M - b.row0 < BM ? a.M - b.row0 : BM);
         b.expert = 0;
-        return true;
-    } else {
-        // lane l adds up the row blocks of experts l run .. l run + run - 1
-        const int lane = threadIdx.x & 63, run = (a.E + 63) / 64;
-        // an expert's rows below the capacity
-        const auto rows_of = [&](int n, int o) {
-            const int most = o < 0 || o > a.capacity ? 0 : a.capacity - o;
-            return n < 0 ? 0 : n > most ? most : n;
-        };
-        int mine = 0;
-#pragma unroll 4
-        for (int i = 0; i < run; ++i) {
-            const int e = lane * run + i;
-            if (e < a.E) mine += (rows_of(a.counts[e], a.offsets[e]) + BM - 1) / BM;
-        }
-        mine = mine < 1 << 24 ? mine : 1 << 24;     // (more than any launch has: the sums stay in 31 bits)
-        const int upto = lanes_before(mine), total = __builtin_amdgcn_readlane(upto, 63);
-        // each chiplet takes a contiguous share of the blocks, an expert's after another's
-        const int64_t all = (int64_t)total * cols, per = (all + kXcds - 1) / kXcds;
-        const int64_t l = p / kXcds, t = (int64_t)(p % kXcds) * per + l;
-        if (l >= per || t >= all) return false;
-        const int at = (int)(t / cols);             // among the experts' row blocks
-        const int owner = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > at));
-        const int before = __builtin_amdgcn_readlane(upto, owner) - __builtin_amdgcn_readlane(mine, owner);
-        // the owner's experts, one to a lane
-        const int e = owner * run + lane;
-        const bool there = lane < run && e < a.E;
-        const int o_mine = there ? a.offsets[e] : 0, n_mine = there ? rows_of(a.counts[e], o_mine) : 0;
-        const int past = before + lanes_before((n_mine + BM - 1) / BM);
-        const int w = __builtin_ctzll(__builtin_amdgcn_ballot_w64(past > at));
-        const int expert = owner * run + w, n = __builtin_amdgcn_readlane(n_mine, w), o = __builtin_amdgcn_readlane(o_mine, w);
-        const int first = __builtin_amdgcn_readlane(past, w) - (n + BM - 1) / BM;
-        // (an expert's row blocks side by side: they share its weights)
-        const int inside = (int)(t - (int64_t)first * cols), high = (n + BM - 1) / BM, r = inside % high * BM;
-        b.expert = expert;
-        b.row0 = (int64_t)o + r;
-        b.col0 = (int64_t)(inside / high) * width;
-        b.rows = n - r < BM ? n - r : BM;
         return true;
     }
 }

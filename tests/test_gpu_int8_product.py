@@ -215,6 +215,57 @@ def test_experts_large_tiles(T, K, E, N, H, gather):
     Experts(T, K, E, N, H, "bf16", gather, align=64, drop=0.05, bias=True).check()
 
 
+@pytest.mark.parametrize("gather", [True, False])
+@pytest.mark.parametrize("N,H,dtype", [(1280, 1024, "bf16"), (1165, 1100, "fp16"), (1408, 1170, "bf16")])
+def test_experts_of_unequal_tiles(N, H, dtype, gather):
+    """More tiles of 256 x 256 than compute units, whole ones, halves and ends in turn; gaps between the experts'
+    rows, rows without a token."""
+    rng = np.random.default_rng(N)
+    counts = np.array([512, 0, 1, 100, 128, 129, 256, 257, 300, 511, 0, 512, 600, 1000, 2000, 2500, 3333, 640, 17, 900, 768, 1100])
+    gaps = rng.integers(0, 4, len(counts) + 1)
+    offsets = (gaps[-1] + np.concatenate([[0], np.cumsum(counts + gaps[:-1])])).astype(np.int32)
+    E, choices, cap = len(counts), 3, int(offsets[-1]) + 5
+    T = cap // choices if gather else cap - 40          # (the last rows are of rows of a that are not there)
+    pairs = rng.integers(0, T * choices, cap).astype(np.int32)
+    pairs[::50] = -1
+    pairs[7::300] = T * choices + 2
+    a, sa, b, sb = codes(rng, T, H), scales(rng, T), codes(rng, E, N, H), scales(rng, E, N)
+    bias = to_dtype(rng.normal(size=(E, N)), dtype)
+    C = Mat(cap, N, dtype)
+    counts = counts.astype(np.int32)
+    fo.int8_experts(Codes(T, H, values=a).whole, dev(sa), Codes(E * N, H, values=b.reshape(E * N, H)).whole, dev(sb), C.t, N, H, E,
+                    dtype, cap, dev(offsets), dev(counts), T, pair_of=dev(pairs) if gather else None, choices=choices,
+                    bias=vec(bias, dtype))
+    want = ref.experts(a, sa, b, sb, offsets, counts, cap, pairs if gather else None, choices, bias)
+    assert C.guards_stand(list(want))
+    v, mag = (np.array([w[i] for w in want.values()]) for i in (0, 1))
+    close(C.values()[list(want)], v, product_bound(v, mag, dtype), "unequal tiles", dtype)
+    bits = C.raw.cpu().numpy()[:cap * N].reshape(cap, N)
+    left = np.setdiff1d(np.arange(cap), list(want))
+    assert len(left) > 30 and (bits[left] == GUARD).all()
+
+
+def test_a_thousand_experts_in_tiles():
+    """As many experts as there may be, with a tile's rows each."""
+    torch = torch_mod()
+    rng = np.random.default_rng(8)
+    E, N, H, dtype = 1024, 130, 300, "bf16"
+    counts = rng.integers(100, 240, E).astype(np.int32)
+    offsets = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    cap = int(offsets[-1])
+    a, sa, b, sb = codes(rng, cap, H), scales(rng, cap), codes(rng, E, N, H), scales(rng, E, N)
+    C = Mat(cap, N, dtype)
+    fo.int8_experts(Codes(cap, H, values=a).whole, dev(sa), Codes(E * N, H, values=b.reshape(E * N, H)).whole, dev(sb), C.t, N, H, E,
+                    dtype, cap, dev(offsets), dev(counts), cap)
+    torch.cuda.synchronize()
+    got = C.values()
+    for e in rng.choice(E, 60, replace=False):
+        rows = slice(offsets[e], offsets[e + 1])
+        want, mag = ref.product(a[rows], sa[rows], b[e], sb[e])
+        close(got[rows], want, product_bound(want, mag, dtype), f"expert {e}", dtype)
+    assert C.guards_stand()
+
+
 @pytest.mark.parametrize("H", [16, 100, 500, 1500])
 def test_experts_several_blocks_to_a_workgroup(H):
     """Short sums and many columns."""
