@@ -431,19 +431,23 @@ Form product_form(int64_t M, int64_t N, int64_t K) {
 // a tile's rows behind the last whole one, half have a half tile): us, bf16, tiles and blocks:
 //   1200 tokens to 8 of 64, 2048 columns  K 7168  280 / 272     1600 tokens  285 / 316
 //   2400 tokens to 8 of 64, 7168 columns  K 2048  389 / 449     4096 tokens, K 512  246 / 307
+//   900 tokens to 8 of 64, 7168 columns   K 2048  245 / 261     600 tokens   233 / 224
+//   4000 tokens to 8 of 256, 7168 columns K 2048  957 / 1089
 //   1000 tokens to 2 of 8,  4096 columns  K 4096   61 /  80     2000 tokens  105 / 106
 //   8192 tokens to 4 of 60, 2881 columns  K 1409  248 / 285     6000 tokens, 300 columns, K 4000  110 / 83
 //   8192 tokens to 1 of 16, 1024 columns  K 1024   23 /  21     1500 to 2 of 16, 1408 columns, K 2048  31 / 19
+//   1316 tokens to 8 of 16, 3648 columns  K 151    41 /  35
 int64_t pairs_of(const Int8Args& a) { return a.pair_of ? std::min<int64_t>(a.capacity, a.a_rows * a.choices) : a.capacity; }
 Form experts_form(const Int8Args& a) {
     const int64_t pairs = pairs_of(a);
     const int64_t experts = std::min<int64_t>(a.E, pairs), each = (pairs + experts - 1) / experts;
     const int64_t steps = (int8_row_bytes(a.K) + 127) / 128;
     const auto blocks = [&](int64_t size) { return experts * ((each + size - 1) / size) * ((a.N + size - 1) / size); };
-    // (the last round of tiles or blocks half full)
+    // (the last round of tiles or blocks half full; without pair_of, rows of padding count as well)
     const double tiles = (double)((a.N + 255) / 256) * ((double)pairs / 256 + 0.28 * (double)experts) / 256 + 0.5;
     const double pieces = (double)((a.N + 127) / 128) * ((double)pairs / 128 + 0.5 * (double)experts) / 512 + 0.5;
-    if (each > 160 && a.K > 0 && 6000 + tiles * (double)(1460 * steps + 4400) < pieces * (double)(1030 * steps + 4000))
+    const int64_t round = std::max<int64_t>(1460 * steps + 4400, 11000);       // (32 MB of results)
+    if (each > (a.pair_of ? 96 : 160) && a.K > 0 && 6000 + tiles * (double)round < pieces * (double)(1030 * steps + 4000))
         return {256, 256, 2, 1, 1};
     if (each > 8 && blocks(128) >= 144) return {128, 128, 2, 1, blocks(128) < 2048 || steps > 8 ? 1 : steps > 2 ? 2 : 4};
     if (blocks(32) > 2048 || (each > 8 && blocks(32) > 512)) return {64, 64, 4, 1, blocks(64) < 6000 || steps > 16 ? 1 : 4};
