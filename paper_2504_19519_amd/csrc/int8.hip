@@ -427,6 +427,8 @@ Form product_form(int64_t M, int64_t N, int64_t K) {
 //                          2048 columns   K 7168  1: 201 / 173 / 177  2: 230 / 179 / 183  4: - / 198 / 189
 //   512 tokens to 8 of 64, 2048 columns   K 2048  1: 70 / 79     2: 85 / 77 / 103
 //   1217 tokens to 4 of 60, 2881 columns  K 1409  1: 94 / 116    2: 95 / 115 / 154   (in tiles 110)
+//   16 tokens to 8 of 256, 2048 columns   K 256   1: 18.8 / 24.7     K 128  1: 16.5 / 23.3
+//   3352 tokens to 6 of 256, 64 columns   K 640   1: 11.3 / 9.2
 // Tiles or blocks of 128, for experts of which each has more rows or fewer than the average (of
 // a tile's rows behind the last whole one, half have a half tile): us, bf16, tiles and blocks:
 //   1200 tokens to 8 of 64, 2048 columns  K 7168  280 / 272     1600 tokens  285 / 316
@@ -449,7 +451,8 @@ Form experts_form(const Int8Args& a) {
     const int64_t round = std::max<int64_t>(1460 * steps + 4400, 11000);       // (32 MB of results)
     if (each > (a.pair_of ? 96 : 160) && a.K > 0 && 6000 + tiles * (double)round < pieces * (double)(1030 * steps + 4000))
         return {256, 256, 2, 1, 1};
-    if (each > 8 && blocks(128) >= 144) return {128, 128, 2, 1, blocks(128) < 2048 || steps > 8 ? 1 : steps > 2 ? 2 : 4};
+    if (each > 8 && a.N > 64 && blocks(128) >= 144) return {128, 128, 2, 1, blocks(128) < 2048 || steps > 8 ? 1 : steps > 2 ? 2 : 4};
+    if (each <= 8 && a.N > 64 && steps <= 2 && blocks(32) > 2048 && blocks(64) < 6000) return {128, 128, 2, 1, 1};
     if (blocks(32) > 2048 || (each > 8 && blocks(32) > 512)) return {64, 64, 4, 1, blocks(64) < 6000 || steps > 16 ? 1 : 4};
     return {32, 32, 4, 1, 1};
 }

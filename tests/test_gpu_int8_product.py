@@ -273,6 +273,15 @@ def test_experts_several_blocks_to_a_workgroup(H):
     Experts(1000, 2, 16, 2300, min(H, 500), "bf16", False).check()
 
 
+@pytest.mark.parametrize("T,K,E,N,H", [(200, 4, 160, 2500, 40), (200, 4, 160, 2530, 300), (200, 4, 160, 2499, 900), (750, 4, 60, 4500, 200),
+                                       (750, 4, 60, 4555, 500), (16, 8, 256, 1100, 130), (500, 4, 200, 64, 70)])
+def test_experts_many_blocks(T, K, E, N, H):
+    """Several blocks to a workgroup, of 64 and of 128 columns, the last one past the columns' end; blocks of 128
+    for a few rows; of 64 for 64 columns."""
+    Experts(T, K, E, N, H, "bf16", True, bias=True, drop=0.1).check()
+    Experts(T, K, E, N, H, "fp16", False).check()
+
+
 def test_experts_rows_apart():
     Experts(50, 2, 6, 37, 100, "bf16", True, lda=128, ldb=160, ldc=45).check()
     Experts(300, 2, 3, 150, 100, "bf16", False, lda=144, ldb=128, ldc=151).check()
