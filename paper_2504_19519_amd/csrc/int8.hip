@@ -389,30 +389,36 @@ struct Form {
 };
 
 // Nanoseconds of a launch of `tiles` 256 x 256 tiles, one to a compute unit, and of `blocks`
-// 128 x 128 blocks, two to a compute unit, of `steps` each. As measured, us in tiles and in
-// blocks: 8192 x 8192 x 8192 393 and 530; 8192 x 8192 x 3584 181 and 231; 4096 x 4096 x 4096 54
-// and 70; 2048 x 4096 x 4096 48 and 34; 4768 x 4736 x 4672 109 and 145; 7596 x 5376 x 192 29 and 34.
+// 128 x 128 blocks, two to a compute unit, of `steps` each; sums of a few steps wait for the
+// results' way out. As measured, us in tiles and in blocks: 8192 x 8192 x 8192 393 and 530;
+// 8192 x 8192 x 3584 181 and 231; 4096 x 4096 x 4096 54 and 70; 2048 x 4096 x 4096 48 and 34;
+// 4768 x 4736 x 4672 109 and 145; 13893 x 15552 x 704 211 and 242; 12162 x 2368 x 2496 72 and 91;
+// 11816 x 6080 x 512 68 and 65, x 128 53 and 43; 7596 x 5376 x 192 35 and 29; 3803 x 6976 x 256
+// 27 and 22.
 int64_t tiles_ns(int64_t tiles, int64_t steps) {
-    const int64_t rest = tiles % 256, round = 1460 * steps + 4400;
+    const int64_t rest = tiles % 256, round = std::max(1460 * steps + 4400, 1100 * steps + 9000);
     return 6000 + tiles / 256 * round + (rest == 0 ? 0 : rest <= 128 ? 1250 * steps + 2000 : round);
 }
 int64_t blocks_ns(int64_t blocks, int64_t steps) {
-    const int64_t rest = blocks % 512;
-    return blocks / 512 * (1030 * steps + 4000) + (rest == 0 ? 0 : rest <= 256 ? 700 * steps + 3000 : 1030 * steps + 4000);
+    const int64_t rest = blocks % 512, round = std::max(1030 * steps + 1500, 850 * steps + 3800);
+    return blocks / 512 * round + (rest == 0 ? 0 : rest <= 256 ? 700 * steps + 3000 : round);
 }
 
 // us, bf16: 1024 x 4096 x 4096 in blocks of 128 with three stages 21, with two 25, of 64 28;
 // 512 x 4096 x 4096 of 64 16, of 128 25; 128 x 4096 x 4096 of 32 9.6, of 64 10.0, 256 x 4096
 // x 4096 15.5 and 10.6; 16 x 14336 x 4096 of 32 11.3, of 64 12.0. In parts: 16 x 256 x 16384
-// 8.7 for 16.0, 128 x 1024 x 16384 13.1 for 18.5, but 16 x 256 x 4096 6.7 for 6.4.
+// 8.7 for 16.0, 128 x 1024 x 16384 13.1 for 18.5, but 16 x 256 x 4096 6.7 for 6.4, 1 x 4096 x 16384
+// 15.8 for 12.0 in the kernel for few blocks.
 Form product_form(int64_t M, int64_t N, int64_t K) {
     const int64_t steps = (int8_row_bytes(K) + 127) / 128;
     const auto blocks = [&](int64_t size) { return ((M + size - 1) / size) * ((N + size - 1) / size); };
-    if (M > 128 && K > 0 && tiles_ns(blocks(256), steps) < blocks_ns(blocks(128), steps)) return {256, 256, 2, 1, 1};
+    // (blocks fare worse where rows share lines of 128 bytes: 5000 x 5000 x 1000 44 us in tiles and 52)
+    const int64_t shared = int8_row_bytes(K) % 128 != 0 ? 23 : 20;
+    if (M > 128 && K > 0 && tiles_ns(blocks(256), steps) < blocks_ns(blocks(128), steps) / 20 * shared) return {256, 256, 2, 1, 1};
     if (M > 40 && blocks(128) > 256) return {128, 128, 2, 1, 1};
     if (M > 40 && blocks(128) >= 144 && steps >= 8) return {128, 128, 3, 1, 1};
     if (M > 32 && blocks(32) > 512) return {64, 64, 4, 1, 1};
-    if (blocks(32) <= 128 && steps >= 64) return {32, 32, 4, 4, 1};
+    if (blocks(32) <= 128 && steps >= 64 && (M > 4 || blocks(16) <= 128)) return {32, 32, 4, 4, 1};
     if (blocks(16) <= 256) return {16, 16, 0, 1, 1};
     return {32, 32, 4, 1, 1};
 }

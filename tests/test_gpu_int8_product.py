@@ -97,6 +97,13 @@ def test_inner_sizes_that_are_split(M, N, K, bias):
     check(M, N, K, "fp16", bias=bias, ldc=N + 5)
 
 
+@pytest.mark.parametrize("M,N,K,bias,ldc", [(5000, 5000, 1000, True, None), (8200, 4097, 1090, False, 4101), (16384, 2304, 2048, True, None),
+                                            (2304, 16384, 2047, False, 16392)])
+def test_tiles_one_after_another(M, N, K, bias, ldc):
+    """Two or three tiles of 256 x 256 to a workgroup, whole ones and ends of rows and columns."""
+    check(M, N, K, "bf16", bias=bias, ldc=ldc)
+
+
 @pytest.mark.parametrize("M", [7, 64])
 def test_weights_past_the_caches(M):
     """More than 128 MiB of weights, in lines of their own, under few rows; and the same of experts."""
@@ -243,6 +250,12 @@ def test_experts_of_unequal_tiles(N, H, dtype, gather):
     bits = C.raw.cpu().numpy()[:cap * N].reshape(cap, N)
     left = np.setdiff1d(np.arange(cap), list(want))
     assert len(left) > 30 and (bits[left] == GUARD).all()
+
+
+@pytest.mark.parametrize("H", [512, 600, 760])
+@pytest.mark.parametrize("gather", [True, False])
+def test_experts_short_sums_in_tiles(H, gather):
+    Experts(4096, 2, 8, 4608, H, "fp16", gather, drop=0.01).check()
 
 
 def test_a_thousand_experts_in_tiles():
