@@ -432,7 +432,7 @@ Form product_form(int64_t M, int64_t N, int64_t K) {
 //   16 tokens to 8 of 256, 7168 columns   K 2048  1: 200 / 202   2: 191 / 185 / 195  4: 188 / 183 / 189
 //                          2048 columns   K 7168  1: 201 / 173 / 177  2: 230 / 179 / 183  4: - / 198 / 189
 //   512 tokens to 8 of 64, 2048 columns   K 2048  1: 70 / 79     2: 85 / 77 / 103
-//   1217 tokens to 4 of 60, 2881 columns  K 1409  1: 94 / 116    2: 95 / 115 / 154   (in tiles 110)
+//   1217 tokens to 4 of 60, 2881 columns  K 1409  1: 94 / 116    2: 95 / 115 / 154   (in tiles 104)
 //   16 tokens to 8 of 256, 2048 columns   K 256   1: 18.8 / 24.7     K 128  1: 16.5 / 23.3
 //   3352 tokens to 6 of 256, 64 columns   K 640   1: 11.3 / 9.2
 // Tiles or blocks of 128, for experts of which each has more rows or fewer than the average (of
