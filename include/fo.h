@@ -693,7 +693,7 @@ fo_status fo_quantize_rows(int32_t dtype, int64_t M, int64_t N, const void* x, i
  * may be NULL: h [M, N], the next residual; y [M, N] of dtype; codes and scales (both
  * or neither), y in 8 bits by fo_quantize_rows' formula, y not rounded to dtype on the
  * way; rstd [M] fp32, for the backward pass. y, or codes and scales, is asked for. h and
- * y may each be x or residual (same ld), and must not overlap otherwise.
+ * y may each be x or residual (same ld); the outputs must not overlap anything else.
  * Magnitudes of h up to 2^60 stay within fp32; products h * gamma are taken as fp32
  * holds them (exact from 2^-126 to 2^128).
  * Errors: FO_ERR_ARG, FO_ERR_UNSUPPORTED, FO_ERR_SHAPE, FO_ERR_HIP.
@@ -722,7 +722,7 @@ fo_status fo_norm_add_backward(int32_t dtype, int64_t M, int64_t N, const void* 
  * + bias[n]: c [M, N] of dtype, a [M, K] and b [N, K] in 8 bits (any codes, -128 too),
  * bias [N] of dtype or NULL. The sum is exact (K <= 131071, else FO_ERR_UNSUPPORTED);
  * it is rounded to fp32, multiplied in this order, and the result rounded to dtype. M, N
- * and K are of any size (K = 0: the bias, or zeros). c must not overlap the others.
+ * and K are of any size (K = 0: the bias, or zeros). c and the workspace must not overlap the others.
  * workspace: fo_int8_workspace_bytes(M, N, K) bytes (0 for most sizes), 16-byte aligned,
  * that no other call uses meanwhile (a graph keeps using it on replay).
  * Errors: FO_ERR_ARG, FO_ERR_UNSUPPORTED, FO_ERR_SHAPE, FO_ERR_HIP.

@@ -24,6 +24,15 @@ fo_status check_codes(const char* what, const void* p, int64_t n, int64_t ld) {
 int64_t extent(int64_t rows, int64_t n, int64_t ld, int64_t bytes) { return rows > 0 && n > 0 ? ((rows - 1) * ld + n) * bytes : 0; }
 int64_t codes_extent(int64_t rows, int64_t n, int64_t ld) { return extent(rows, int8_row_bytes(n), ld, 1); }
 
+struct Piece {
+    const void* p;
+    int64_t bytes;
+};
+template <size_t N>
+bool overlaps(const Piece& a, const Piece (&others)[N]) {
+    return std::any_of(others, others + N, [&](const Piece& b) { return overlap(a.p, a.bytes, b.p, b.bytes); });
+}
+
 fo_status check_scales(const char* what, const void* p) {
     if (!p) return fail(FO_ERR_ARG, std::string(what) + " is NULL");
     if (!aligned(p, 4)) return fail(FO_ERR_ARG, std::string(what) + " must be 4-byte aligned");
@@ -104,10 +113,15 @@ fo_status fo_norm_add_forward(int32_t dtype, int64_t M, int64_t N, const void* x
         fo::clash(x, M, ldx, y, M, ldy, N, true) || fo::clash(residual, M, ldr, y, M, ldy, N, true))
         return fo::fail(FO_ERR_ARG, "h or y overlaps x or residual without being it");
     if (fo::clash(h, M, ldh, y, M, ldy, N, false)) return fo::fail(FO_ERR_ARG, "h and y overlap");
-    const int64_t nc = fo::codes_extent(M, N, ldc);
-    if (fo::overlap(codes, nc, x, fo::extent(M, N, ldx, 2)) || fo::overlap(codes, nc, residual, fo::extent(M, N, ldr, 2)) ||
-        fo::overlap(codes, nc, h, fo::extent(M, N, ldh, 2)) || fo::overlap(codes, nc, y, fo::extent(M, N, ldy, 2)))
-        return fo::fail(FO_ERR_ARG, "codes overlaps another matrix");
+    if (fo::overlap(gamma, 2 * N, h, fo::extent(M, N, ldh, 2)) || fo::overlap(gamma, 2 * N, y, fo::extent(M, N, ldy, 2)))
+        return fo::fail(FO_ERR_ARG, "h or y overlaps gamma");
+    const fo::Piece out[] = {{codes, fo::codes_extent(M, N, ldc)}, {scales, 4 * M}, {rstd, 4 * M}};
+    const fo::Piece others[] = {{x, fo::extent(M, N, ldx, 2)}, {residual, fo::extent(M, N, ldr, 2)}, {h, fo::extent(M, N, ldh, 2)},
+                                {y, fo::extent(M, N, ldy, 2)}, {gamma, 2 * N}};
+    for (int i = 0; i < 3; ++i) {
+        if (fo::overlaps(out[i], others) || fo::overlap(out[i].p, out[i].bytes, out[(i + 1) % 3].p, out[(i + 1) % 3].bytes))
+            return fo::fail(FO_ERR_ARG, "codes, scales or rstd overlaps another argument");
+    }
     fo::Rows8Args a{};
     a.x = static_cast<const uint16_t*>(x);
     a.residual = static_cast<const uint16_t*>(residual);
@@ -175,13 +189,15 @@ fo_status fo_int8_product(int32_t dtype, int64_t M, int64_t N, int64_t K, const 
     if ((st = fo::check_product(dtype, M, N, K)) != FO_OK) return st;
     if (M == 0 || N == 0) return FO_OK;
     if ((st = fo::check_operands(a, a_scales, lda, b, b_scales, ldb, bias, c, ldc, N, K)) != FO_OK) return st;
-    const int64_t nc = fo::extent(M, N, ldc, 2);
-    if (fo::overlap(c, nc, a, fo::codes_extent(M, K, lda)) || fo::overlap(c, nc, b, fo::codes_extent(N, K, ldb)) ||
-        fo::overlap(c, nc, bias, 2 * N))
-        return fo::fail(FO_ERR_ARG, "c overlaps an operand");
     const int64_t need = fo_int8_workspace_bytes(M, N, K);
     if (need > 0 && (!workspace || !fo::aligned(workspace, 16) || workspace_bytes < need))
         return fo::fail(FO_ERR_ARG, "workspace: fo_int8_workspace_bytes(M, N, K) bytes, 16-byte aligned");
+    const fo::Piece out = {c, fo::extent(M, N, ldc, 2)}, space = {workspace, need};
+    const fo::Piece others[] = {{a, fo::codes_extent(M, K, lda)}, {b, fo::codes_extent(N, K, ldb)}, {a_scales, 4 * M},
+                                {b_scales, 4 * N}, {bias, 2 * N}};
+    if (fo::overlaps(out, others)) return fo::fail(FO_ERR_ARG, "c overlaps an operand");
+    if (fo::overlaps(space, others) || fo::overlap(c, out.bytes, workspace, need))
+        return fo::fail(FO_ERR_ARG, "the workspace overlaps another argument");
     fo::Int8Args p{};
     p.a = static_cast<const int8_t*>(a);
     p.a_scales = a_scales;
@@ -213,10 +229,11 @@ fo_status fo_int8_experts(int32_t dtype, int64_t capacity, int64_t N, int64_t K,
     if (a_rows > INT32_MAX || E * N > INT32_MAX) return fo::fail(FO_ERR_SHAPE, "2^31 rows or more");
     if (pair_of && K > 0 && fo::codes_extent(a_rows, K, lda) > (int64_t)1 << 31)
         return fo::fail(FO_ERR_SHAPE, "rows taken through pair_of from more than 2^31 bytes");
-    const int64_t nc = fo::extent(capacity, N, ldc, 2);
-    if (fo::overlap(c, nc, a, fo::codes_extent(a_rows, K, lda)) || fo::overlap(c, nc, b, fo::codes_extent(E * N, K, ldb)) ||
-        fo::overlap(c, nc, bias, 2 * E * N))
-        return fo::fail(FO_ERR_ARG, "c overlaps an operand");
+    const fo::Piece out = {c, fo::extent(capacity, N, ldc, 2)};
+    const fo::Piece others[] = {{a, fo::codes_extent(a_rows, K, lda)}, {b, fo::codes_extent(E * N, K, ldb)}, {a_scales, 4 * a_rows},
+                                {b_scales, 4 * E * N}, {bias, 2 * E * N}, {pair_of, 4 * capacity}, {offsets, 4 * (E + 1)},
+                                {counts, 4 * E}};
+    if (fo::overlaps(out, others)) return fo::fail(FO_ERR_ARG, "c overlaps an operand");
     fo::Int8Args p{};
     p.a = static_cast<const int8_t*>(a);
     p.a_scales = a_scales;

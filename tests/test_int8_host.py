@@ -171,3 +171,30 @@ def test_reference_products():
     assert sorted(got) == [0, 1, 4]           # row 5: token 6 of 6
     for r, s, e in ((0, 1, 0), (1, 5, 0), (4, 0, 2)):
         np.testing.assert_allclose(got[r][0], ref.product(a[s:s + 1], sa[s:s + 1], b[e], sb[e], bias[e])[0][0])
+
+
+def test_outputs_that_overlap_other_arguments():
+    """A scale, a bias or a place that a call would overwrite while it reads it."""
+    def norm(x=P, residual=2 * P, gamma=None, h=3 * P, y=4 * P, codes=5 * P, scales=6 * P, rstd=7 * P):
+        fo.norm_add_forward(x, residual, gamma, h, y, 4, 70, "bf16", codes=codes, scales=scales, rstd=rstd)
+    for bad in (dict(rstd=6 * P), dict(rstd=6 * P + 12), dict(scales=5 * P + 16), dict(rstd=5 * P), dict(scales=P), dict(scales=2 * P + 4),
+                dict(rstd=3 * P), dict(rstd=4 * P + 8), dict(gamma=3 * P + 2), dict(gamma=4 * P), dict(gamma=6 * P), dict(gamma=5 * P)):
+        refused(ARG, norm, **bad)
+
+    M, N, K = 4, 40, 8192
+    need = fo.int8_workspace_bytes(M, N, K)
+    assert need > 0
+
+    def product(a=P, a_scales=2 * P, b=3 * P, b_scales=4 * P, bias=5 * P, c=6 * P, workspace=7 * P):
+        fo.int8_product(a, a_scales, b, b_scales, c, M, N, K, "fp16", bias=bias, workspace=workspace)
+    for bad in (dict(c=2 * P), dict(c=4 * P + 16), dict(c=5 * P), dict(c=3 * P + 32), dict(c=7 * P), dict(c=7 * P + need - 2),
+                dict(workspace=P), dict(workspace=2 * P), dict(workspace=3 * P + 16), dict(workspace=4 * P), dict(workspace=5 * P)):
+        refused(ARG, product, **bad)
+
+    E, cap, rows = 3, 12, 5
+
+    def experts(a=P, a_scales=2 * P, b=3 * P, b_scales=4 * P, bias=5 * P, c=6 * P, offsets=7 * P, counts=8 * P, pair_of=9 * P):
+        fo.int8_experts(a, a_scales, b, b_scales, c, N, 64, E, "fp16", cap, offsets, counts, rows, pair_of=pair_of, choices=2, bias=bias)
+    for at in (dict(a=6 * P), dict(a_scales=6 * P + 4), dict(b=6 * P + 16), dict(b_scales=6 * P), dict(bias=6 * P), dict(offsets=6 * P),
+               dict(counts=6 * P + 8), dict(pair_of=6 * P + 4)):
+        refused(ARG, experts, **at)
