@@ -34,7 +34,7 @@ namespace {
 // 157 us, 6.3 TB/s), else by waits for LDS and by MFMAs (1024 x 4096 x 4096 21 us, 1.6 POPS).
 constexpr int kNontemporal = 2;         // cache policy of a buffer load
 template <int DT, int BM, int BN, int ST, bool EXPERTS, bool ONCE>
-__global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 ? 1 : 2) void int8_block_kernel(const Int8Args a) {
+__global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 && BN == 128 ? 1 : 2) void int8_block_kernel(const Int8Args a) {
     constexpr int kWaves = 4, WTM = BM / 2, WTN = BN / 2, MI = WTM / 16, NJ = WTN / 16;
     constexpr int kA = BM * 128, kStage = (BM + BN) * 128;
     constexpr int kAI = kA / 1024 / kWaves, kBI = BN * 128 / 1024 / kWaves, kLoads = kAI + kBI;
@@ -404,11 +404,13 @@ int64_t blocks_ns(int64_t blocks, int64_t steps) {
     return blocks / 512 * round + (rest == 0 ? 0 : rest <= 256 ? 700 * steps + 3000 : round);
 }
 
-// us, bf16: 1024 x 4096 x 4096 in blocks of 128 with three stages 21, with two 25, of 64 28;
-// 512 x 4096 x 4096 of 64 16, of 128 25; 128 x 4096 x 4096 of 32 9.6, of 64 10.0, 256 x 4096
-// x 4096 15.5 and 10.6; 16 x 14336 x 4096 of 32 11.3, of 64 12.0. In parts: 16 x 256 x 16384
-// 8.7 for 16.0, 128 x 1024 x 16384 13.1 for 18.5, but 16 x 256 x 4096 6.7 for 6.4, 1 x 4096 x 16384
-// 15.8 for 12.0 in the kernel for few blocks.
+// us, bf16: 1024 x 4096 x 4096 in blocks of 128 with three stages 21, with two 25, of 64 28; 512 x
+// 4096 x 4096 of 64 15.8, of 128 25, of 128 x 64 13.8; 333 x 2881 x 1985 of 64 12.0, of 128 x 64
+// 10.3; 1024 x 2048 x 7168 26 and 21, but 256 x 4096 x 4096, where those of 64 are one to a compute
+// unit, 9.8 and 12.9; 128 x 4096 x 4096 of 32 9.6, of 64 10.0, 256 x 4096 x 4096 15.5 and 10.6; 16 x
+// 14336 x 4096 of 32 11.3, of 64 12.0. In parts: 16 x 256 x 16384 8.7 for 16.0, 128 x 1024 x 16384
+// 13.1 for 18.5, but 16 x 256 x 4096 6.7 for 6.4, 1 x 4096 x 16384 15.8 for 12.0 in the kernel for
+// few blocks.
 Form product_form(int64_t M, int64_t N, int64_t K) {
     const int64_t steps = (int8_row_bytes(K) + 127) / 128;
     const auto blocks = [&](int64_t size) { return ((M + size - 1) / size) * ((N + size - 1) / size); };
@@ -417,6 +419,7 @@ Form product_form(int64_t M, int64_t N, int64_t K) {
     if (M > 128 && K > 0 && tiles_ns(blocks(256), steps) < blocks_ns(blocks(128), steps) / 20 * shared) return {256, 256, 2, 1, 1};
     if (M > 40 && blocks(128) > 256) return {128, 128, 2, 1, 1};
     if (M > 40 && blocks(128) >= 144 && steps >= 8) return {128, 128, 3, 1, 1};
+    if (M > 64 && blocks(64) > 256) return {128, 64, 3, 1, 1};
     if (M > 32 && blocks(32) > 512) return {64, 64, 4, 1, 1};
     if (blocks(32) <= 128 && steps >= 64 && (M > 4 || blocks(16) <= 128)) return {32, 32, 4, 4, 1};
     if (blocks(16) <= 256) return {16, 16, 0, 1, 1};
@@ -483,7 +486,7 @@ hipError_t launch_any(int dtype, const Int8Args& a, const Form& f, hipStream_t s
     const dim3 grid((uint32_t)blocks_of<EXPERTS>(a, f.rows, f.cols * f.span), (uint32_t)f.parts);
     const auto block = [&](auto bm, auto bn, auto st) {
         constexpr int BM = decltype(bm)::value, BN = decltype(bn)::value, ST = decltype(st)::value;
-        if constexpr (BM <= 64) {
+        if constexpr (BN <= 64) {
             if (weights_once(a, f, EXPERTS))
                 return launch(dtype == FO_FP16 ? int8_block_kernel<FO_FP16, BM, BN, ST, EXPERTS, true>
                                                : int8_block_kernel<FO_BF16, BM, BN, ST, EXPERTS, true>, grid, 256, s, a);
@@ -493,6 +496,7 @@ hipError_t launch_any(int dtype, const Int8Args& a, const Form& f, hipStream_t s
     };
     if (f.rows == 256) return launch_int8_tile(dtype, EXPERTS, grid.x, a, s);
     if constexpr (!EXPERTS) {
+        if (f.cols == 64 && f.rows == 128) return block(Int<128>(), Int<64>(), Int<3>());
         if (f.rows == 128 && f.stages == 3) return block(Int<128>(), Int<128>(), Int<3>());
     }
     if (f.rows == 128) return block(Int<128>(), Int<128>(), Int<2>());

@@ -104,6 +104,14 @@ def test_tiles_one_after_another(M, N, K, bias, ldc):
     check(M, N, K, "bf16", bias=bias, ldc=ldc)
 
 
+@pytest.mark.parametrize("M,N,K,bias", [(70, 9000, 100, True), (129, 8200, 40, False), (333, 2881, 1985, True), (513, 2050, 1300, False),
+                                        (1000, 1100, 16, True), (128, 16384, 260, False), (100, 16500, 8192, True)])
+def test_blocks_of_two_to_one(M, N, K, bias):
+    """Blocks of 128 rows and 64 columns; the last ones' weights past the caches' keeping."""
+    check(M, N, K, "bf16", bias=bias, ldc=N + 2)
+    check(M, N, K, "fp16", bias=not bias, lda=row_bytes(K) + 32)
+
+
 @pytest.mark.parametrize("M", [7, 64])
 def test_weights_past_the_caches(M):
     """More than 128 MiB of weights, in lines of their own, under few rows; and the same of experts."""
