@@ -407,8 +407,8 @@ int64_t blocks_ns(int64_t blocks, int64_t steps) {
 // us, bf16: 1024 x 4096 x 4096 in blocks of 128 with three stages 21, with two 25, of 64 28; 512 x
 // 4096 x 4096 of 64 15.8, of 128 25, of 128 x 64 13.8; 333 x 2881 x 1985 of 64 12.0, of 128 x 64
 // 10.3; 1024 x 2048 x 7168 26 and 21, but 256 x 4096 x 4096, where those of 64 are one to a compute
-// unit, 9.8 and 12.9; 128 x 4096 x 4096 of 32 9.6, of 64 10.0, 256 x 4096 x 4096 15.5 and 10.6; 16 x
-// 14336 x 4096 of 32 11.3, of 64 12.0. In parts: 16 x 256 x 16384 8.7 for 16.0, 128 x 1024 x 16384
+// unit, 9.8 and 12.9; 128 x 4096 x 4096 of 32 9.4, of 64 9.5, of 64 x 32 8.7, 64 x 8192 x 1024 5.0,
+// 4.9 and 4.6, 256 x 4096 x 4096 15.5, 10.6 and 12.3; 16 x 14336 x 4096 of 32 11.3, of 64 12.0. In parts: 16 x 256 x 16384 8.7 for 16.0, 128 x 1024 x 16384
 // 13.1 for 18.5, but 16 x 256 x 4096 6.7 for 6.4, 1 x 4096 x 16384 15.8 for 12.0 in the kernel for
 // few blocks.
 Form product_form(int64_t M, int64_t N, int64_t K) {
@@ -421,6 +421,7 @@ Form product_form(int64_t M, int64_t N, int64_t K) {
     if (M > 40 && blocks(128) >= 144 && steps >= 8) return {128, 128, 3, 1, 1};
     if (M > 64 && blocks(64) > 256) return {128, 64, 3, 1, 1};
     if (M > 32 && blocks(32) > 512) return {64, 64, 4, 1, 1};
+    if (M > 32 && blocks(32) > 256) return {64, 32, 4, 1, 1};
     if (blocks(32) <= 128 && steps >= 64 && (M > 4 || blocks(16) <= 128)) return {32, 32, 4, 4, 1};
     if (blocks(16) <= 256) return {16, 16, 0, 1, 1};
     return {32, 32, 4, 1, 1};
@@ -500,8 +501,9 @@ hipError_t launch_any(int dtype, const Int8Args& a, const Form& f, hipStream_t s
         if (f.rows == 128 && f.stages == 3) return block(Int<128>(), Int<128>(), Int<3>());
     }
     if (f.rows == 128) return block(Int<128>(), Int<128>(), Int<2>());
-    if (f.rows == 64) return block(Int<64>(), Int<64>(), Int<4>());
+    if (f.cols == 64) return block(Int<64>(), Int<64>(), Int<4>());
     if constexpr (!EXPERTS) {
+        if (f.rows == 64) return block(Int<64>(), Int<32>(), Int<4>());
         if (f.rows == 16)
             return launch(dtype == FO_FP16 ? int8_few_kernel<FO_FP16> : int8_few_kernel<FO_BF16>, grid, 256, s, a);
     }

@@ -105,9 +105,10 @@ def test_tiles_one_after_another(M, N, K, bias, ldc):
 
 
 @pytest.mark.parametrize("M,N,K,bias", [(70, 9000, 100, True), (129, 8200, 40, False), (333, 2881, 1985, True), (513, 2050, 1300, False),
-                                        (1000, 1100, 16, True), (128, 16384, 260, False), (100, 16500, 8192, True)])
+                                        (1000, 1100, 16, True), (128, 16384, 260, False), (33, 4500, 100, False), (64, 8192, 16, True), (100, 3001, 1000, True),
+                                        (257, 1500, 700, False), (64, 4200, 32768, True), (100, 16500, 8192, True)])
 def test_blocks_of_two_to_one(M, N, K, bias):
-    """Blocks of 128 rows and 64 columns; the last ones' weights past the caches' keeping."""
+    """Blocks of 128 rows and 64 columns, and of 64 and 32; the last ones' weights past the caches' keeping."""
     check(M, N, K, "bf16", bias=bias, ldc=N + 2)
     check(M, N, K, "fp16", bias=not bias, lda=row_bytes(K) + 32)
 
