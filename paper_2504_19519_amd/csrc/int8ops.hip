@@ -159,9 +159,17 @@ fo_status fo_norm_add_backward(int32_t dtype, int64_t M, int64_t N, const void* 
         if (fo::clash(dx, M, lddx, dy, M, lddy, N, true) || fo::clash(dx, M, lddx, dh, M, lddh, N, true) ||
             fo::clash(dx, M, lddx, h, M, ldh, N, true))
             return fo::fail(FO_ERR_ARG, "dx overlaps dy, dh or h without being it");
-        if ((dgamma || fo::norm_dots_bytes(M, N) > 0) &&
-            (!workspace || !fo::aligned(workspace, 16) || workspace_bytes < fo_norm_workspace_bytes(M, N)))
+        const int64_t need = dgamma || fo::norm_dots_bytes(M, N) > 0 ? fo_norm_workspace_bytes(M, N) : 0;
+        if (need > 0 && (!workspace || !fo::aligned(workspace, 16) || workspace_bytes < need))
             return fo::fail(FO_ERR_ARG, "workspace: fo_norm_workspace_bytes(M, N) bytes, 16-byte aligned");
+        const fo::Piece read[] = {{dy, fo::extent(M, N, lddy, 2)}, {dx ? dh : nullptr, fo::extent(M, N, lddh, 2)},
+                                  {h, fo::extent(M, N, ldh, 2)}, {gamma, 2 * N}, {rstd, 4 * M}};
+        const fo::Piece into = {dx, fo::extent(M, N, lddx, 2)}, sums = {dgamma, 4 * N}, space = {workspace, need};
+        const fo::Piece beside[] = {{gamma, 2 * N}, {rstd, 4 * M}, sums, space};        // (the matrices: above)
+        if (fo::overlaps(into, beside)) return fo::fail(FO_ERR_ARG, "dx overlaps gamma, rstd, dgamma or the workspace");
+        if (fo::overlaps(sums, read) || fo::overlap(dgamma, sums.bytes, workspace, need))
+            return fo::fail(FO_ERR_ARG, "dgamma overlaps an input or the workspace");
+        if (fo::overlaps(space, read)) return fo::fail(FO_ERR_ARG, "the workspace overlaps an input");
     }
     fo::NormAddArgs a{};
     a.dy = static_cast<const uint16_t*>(dy);
