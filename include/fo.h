@@ -676,9 +676,10 @@ int64_t fo_int8_row_bytes(int64_t N);
 /*
  * fo_quantize_rows -- per row of x [M, N] (any N up to 2^30): with m the row's largest
  * magnitude, scale = m / 127 and code = 127 x / m, rounded to nearest even. A row of
- * zeros has scale 0; a row with an infinity or a NaN has scale NaN and codes 0, and
- * reads as NaN throughout. Weights (a row for each channel) are put into 8 bits by the
- * same call. codes, scales and x must not overlap.
+ * zeros, or of no values (N = 0; x and codes may be NULL then), has scale 0; a row with
+ * an infinity or a NaN has scale NaN and codes 0, and reads as NaN throughout. Weights (a
+ * row for each channel) are put into 8 bits by the same call. codes, scales and x must not
+ * overlap.
  * Errors: FO_ERR_ARG, FO_ERR_SHAPE, FO_ERR_HIP.
  */
 fo_status fo_quantize_rows(int32_t dtype, int64_t M, int64_t N, const void* x, int64_t ldx, void* codes, int64_t ldc,
@@ -692,8 +693,9 @@ fo_status fo_quantize_rows(int32_t dtype, int64_t M, int64_t N, const void* x, i
  * (RMS norm of h as it is kept). gamma: [N] of dtype, NULL = 1. Outputs, each of which
  * may be NULL: h [M, N], the next residual; y [M, N] of dtype; codes and scales (both
  * or neither), y in 8 bits by fo_quantize_rows' formula, y not rounded to dtype on the
- * way; rstd [M] fp32, for the backward pass. y, or codes and scales, is asked for. h and
- * y may each be x or residual (same ld); the outputs must not overlap anything else.
+ * way; rstd [M] fp32, for the backward pass. y, or codes and scales, is asked for (of N = 0
+ * scales alone are written). h and y may each be x or residual (same ld); the outputs must
+ * not overlap anything else.
  * Magnitudes of h up to 2^60 stay within fp32; products h * gamma are taken as fp32
  * holds them (exact from 2^-126 to 2^128).
  * Errors: FO_ERR_ARG, FO_ERR_UNSUPPORTED, FO_ERR_SHAPE, FO_ERR_HIP.

@@ -39,6 +39,19 @@ fo_status check_scales(const char* what, const void* p) {
     return FO_OK;
 }
 
+// The scales of M rows without values: zeros.
+fo_status no_values(int32_t dtype, int64_t M, float* scales, void* stream) {
+    if (!scales) return FO_OK;
+    if (M > INT32_MAX) return fail(FO_ERR_SHAPE, "2^31 rows or more");
+    fo_status st;
+    if ((st = check_scales("scales", scales)) != FO_OK) return st;
+    Rows8Args a{};
+    a.scales = scales;
+    a.M = M;
+    a.scale = 1.0f;
+    return done(launch_quantize(dtype, a, (hipStream_t)stream), "quantize launch");
+}
+
 fo_status check_product(int32_t dtype, int64_t rows, int64_t N, int64_t K) {
     if (!is_dtype(dtype)) return fail(FO_ERR_ARG, "bad dtype");
     if (rows < 0 || N < 0 || K < 0) return fail(FO_ERR_ARG, "negative size");
@@ -71,7 +84,8 @@ fo_status fo_quantize_rows(int32_t dtype, int64_t M, int64_t N, const void* x, i
     fo_status st;
     if (!fo::is_dtype(dtype)) return fo::fail(FO_ERR_ARG, "bad dtype");
     if (M < 0 || N < 0) return fo::fail(FO_ERR_ARG, "negative size");
-    if (M == 0 || N == 0) return FO_OK;
+    if (M == 0) return FO_OK;
+    if (N == 0) return fo::no_values(dtype, M, scales, stream);
     if (M > INT32_MAX || N > (int64_t)1 << 30) return fo::fail(FO_ERR_SHAPE, "2^31 rows or more, or rows of more than 2^30 values");
     if ((st = fo::check_rows("x", x, N, ldx)) != FO_OK) return st;
     if (!codes) return fo::fail(FO_ERR_ARG, "codes is NULL");
@@ -99,7 +113,8 @@ fo_status fo_norm_add_forward(int32_t dtype, int64_t M, int64_t N, const void* x
     if (M < 0 || N < 0) return fo::fail(FO_ERR_ARG, "negative size");
     if (!(eps >= 0.0f)) return fo::fail(FO_ERR_ARG, "eps must be >= 0");
     if (N > fo::kMaxNormCols) return fo::fail(FO_ERR_UNSUPPORTED, "rows of more than 32768 columns");
-    if (M == 0 || N == 0) return FO_OK;
+    if (M == 0) return FO_OK;
+    if (N == 0) return fo::no_values(dtype, M, scales, stream);
     if (M > INT32_MAX) return fo::fail(FO_ERR_SHAPE, "2^31 rows or more");
     if (!y && !codes && !scales) return fo::fail(FO_ERR_ARG, "no output asked for: y, or codes and scales");
     if ((st = fo::check_rows("x", x, N, ldx)) != FO_OK || (residual && (st = fo::check_rows("residual", residual, N, ldr)) != FO_OK) ||

@@ -77,7 +77,7 @@ __device__ __forceinline__ float first_max(float v) {
 
 // The chunks of eight of a row of n values: chunk c starts at column 8 c, the last one at
 // n - 8 (so that `twice` of its values are the chunk's before it as well). SMALL: rows of
-// fewer than eight values, which have one, read and written in parts.
+// fewer than eight values, which have one, read and written in parts (of none: no chunk).
 template <bool SMALL>
 struct RowChunks {
     int n, last, twice;
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(TH < 64 ? 64 : TH, 4) void rows8_kernel(const Rows8
             if constexpr (NORM) {
                 if (a.rstd) a.rstd[i] = rstd;
             }
-            if (a.codes) a.scales[i] = codes.finite ? over_127(m * rstd) : __builtin_nanf("");
+            if (!NORM || a.codes) a.scales[i] = codes.finite ? over_127(m * rstd) : __builtin_nanf("");
         }
 #pragma unroll
         for (int t = 0; t < CH; ++t) {
