@@ -724,7 +724,8 @@ fo_status fo_norm_add_backward(int32_t dtype, int64_t M, int64_t N, const void* 
  * + bias[n]: c [M, N] of dtype, a [M, K] and b [N, K] in 8 bits (any codes, -128 too),
  * bias [N] of dtype or NULL. The sum is exact (K <= 131071, else FO_ERR_UNSUPPORTED);
  * it is rounded to fp32, multiplied in this order, and the result rounded to dtype. M, N
- * and K are of any size (K = 0: the bias, or zeros). c and the workspace must not overlap the others.
+ * and K are of any size (K = 0: the bias, or zeros, whatever the scales are). c and the
+ * workspace must not overlap the others.
  * workspace: fo_int8_workspace_bytes(M, N, K) bytes (0 for most sizes), 16-byte aligned,
  * that no other call uses meanwhile (a graph keeps using it on replay).
  * Errors: FO_ERR_ARG, FO_ERR_UNSUPPORTED, FO_ERR_SHAPE, FO_ERR_HIP.

@@ -68,7 +68,8 @@ __global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 && BN == 128 ? 1 : 2) v
     const int8_t* const ablk = gather ? a.a : a.a + b.row0 * a.lda;
 
     // What the epilogue wants to know of the rows and columns, a row and a column to a thread:
-    // looked up ahead of the operands' loads, in LDS by the first steps.
+    // looked up ahead of the operands' loads, in LDS by the first steps. (Of K = 0 the scales
+    // count as 0: they may be anything, and the sums are 0.)
     __shared__ int s_from[EXPERTS ? BM : 1];             // row of a, or -1
     __shared__ __attribute__((aligned(16))) float s_row[BM], s_scale[BN], s_bias[BN];
     const int tid = threadIdx.x;
@@ -76,12 +77,12 @@ __global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 && BN == 128 ? 1 : 2) v
     if (tid < BM) {
         const int64_t from = source_row<EXPERTS>(a, b, tid);
         if constexpr (EXPERTS) s_from[tid] = (int)from;
-        if (from >= 0) row_scale = a.a_scales[from];
+        if (from >= 0 && a.K > 0) row_scale = a.a_scales[from];
     }
     auto look_up = [&]() {
         const int64_t n = b.col0 + tid, at = (int64_t)b.expert * a.N + n;
         if (tid < BN && n < a.N) {
-            col_scale = a.b_scales[at];
+            if (a.K > 0) col_scale = a.b_scales[at];
             if (a.bias) col_bias = to_f32<DT>(a.bias[at]);
         }
     };
@@ -351,7 +352,7 @@ __global__ __launch_bounds__(256) void int8_few_kernel(const Int8Args a) {
     if (wave != 0 || r >= b.rows || n >= a.N) return;
     const i32x4_t sum = (s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane]);
     const Columns of = columns_of<DT>(a, n);
-    const u32x2_t v = finish<DT>(sum, a.a_scales[b.row0 + r], of.scale, of.bias);
+    const u32x2_t v = finish<DT>(sum, a.K > 0 ? a.a_scales[b.row0 + r] : 0.0f, of.scale, of.bias);
     write_four(a.c + (b.row0 + r) * a.ldc + n, v, a.N - n);
 }
 

@@ -156,7 +156,7 @@ __device__ __forceinline__ int64_t source_row(const Int8Args& a, const Block& b,
     }
 }
 
-// The scales and bias of columns n .. n + 3 (not by experts).
+// The scales (of K = 0: zeros) and bias of columns n .. n + 3 (not by experts).
 struct Columns {
     f32x4_t scale, bias;
 };
@@ -166,7 +166,7 @@ __device__ __forceinline__ Columns columns_of(const Int8Args& a, int64_t n) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const bool there = n + e < a.N;
-        c.scale[e] = there ? a.b_scales[n + e] : 0.0f;
+        c.scale[e] = there && a.K > 0 ? a.b_scales[n + e] : 0.0f;
         c.bias[e] = there && a.bias ? to_f32<DT>(a.bias[n + e]) : 0.0f;
     }
     return c;
