@@ -6,11 +6,9 @@
 #include <stdint.h>
 
 #include "fo_internal.h"
+#include "int8_form.h"
 
 namespace fo {
-
-// Bytes of a row of n codes: whole chunks of 16.
-FO_HD inline int64_t int8_row_bytes(int64_t n) { return (n + 15) / 16 * 16; }
 
 struct Rows8Args {
     const uint16_t* x;          // [M] rows, ldx apart
@@ -42,28 +40,6 @@ struct NormAddArgs {
 // The sums over rows go to a.partial; then dgamma (or null) is their sum.
 hipError_t launch_norm_add_backward(int dtype, const NormAddArgs& a, float* dgamma, hipStream_t s);
 
-// c = (a b^T) a_scales b_scales + bias: sums in 32-bit integers, exact.
-constexpr int64_t kMaxInt8Inner = 131071;          // 2^14 times as much fits 31 bits
-constexpr int64_t kMaxInt8Row = 1 << 22;           // bytes from row to row: a tile's rows within 31 bits
-struct Int8Args {
-    const int8_t* a;            // rows, lda apart
-    const float* a_scales;
-    const int8_t* b;            // [N] rows, ldb apart; experts: [E * N]
-    const float* b_scales;      // [N]; [E * N]
-    const uint16_t* bias;       // [N]; [E * N]; or null
-    uint16_t* c;                // rows, ldc apart
-    int32_t* partial;           // [parts][M][partial_cols(N)] sums over a part of K each, where it is split
-    int64_t M, N, K, lda, ldb, ldc;
-    // by experts: expert e's rows of c are offsets[e] .. offsets[e] + counts[e] - 1
-    const int32_t* offsets;
-    const int32_t* counts;
-    const int32_t* pair_of;     // row r is of a's row pair_of[r] / choices; null: a's row r
-    int64_t a_rows;
-    int32_t E, choices, capacity;
-    int32_t parts;              // of K; 1: not split
-    int32_t span;               // blocks, side by side, of a workgroup
-    int32_t blocks;             // 256 x 256 tiles, of all workgroups
-};
 int64_t int8_workspace_bytes(int64_t M, int64_t N, int64_t K);
 // Whether a launch takes the product (work-items are counted in 32 bits).
 bool int8_launchable(const Int8Args& a, bool experts);
