@@ -106,3 +106,11 @@ EXPERTS = [
 def expert_rows(T, K, E, align):
     """fo_route_capacity."""
     return T * K + min(E, T * K) * (align - 1)
+
+
+# The longest sums, K = 131071, undivided but for the one in parts: the form, M, N.
+LONGEST = [("few", 4, 2100), ("32x32/4 once", 20, 4200), ("32x32/4 parts 4", 40, 20), ("64x32/4 once", 60, 4200), ("64x64/4 once", 40, 8300),
+           ("128x64/3 once", 100, 8300), ("128x128/3", 1500, 1600), ("128x128/2", 2100, 2100), ("tile", 2560, 4000)]
+# by experts: the form, rows of each, N
+LONGEST_EXPERTS = [("32x32/4 span 1", (5, 0, 3), 200), ("32x32/4 span 1 once", (20, 30, 1), 700), ("128x128/2 span 1", (700, 0, 800), 1500), ("tile", (2500, 60), 3300),
+                   ("64x64/4 span 1 once", (1,) * 40, 1700)]

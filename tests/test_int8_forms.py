@@ -23,6 +23,13 @@ def test_experts(rules, form, T, K, E, N, H, gather, align, ldb):
     assert rules.experts(rows, N, H, E, T if gather else rows, K, gather, ldb) == form
 
 
+def test_longest_sums(rules):
+    for form, M, N in forms.LONGEST:
+        assert rules.product(M, N, 131071) == form, (M, N)
+    for form, counts, N in forms.LONGEST_EXPERTS:
+        assert rules.experts(sum(counts), N, 131071, len(counts), sum(counts), 1, False) == form, (counts, N)
+
+
 def test_no_form_is_left_out(rules):
     """Every form of sizes spread over the whole range (over their logarithms)."""
     rng = random.Random(0)
