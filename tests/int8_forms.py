@@ -114,3 +114,7 @@ LONGEST = [("few", 4, 2100), ("32x32/4 once", 20, 4200), ("32x32/4 parts 4", 40,
 # by experts: the form, rows of each, N
 LONGEST_EXPERTS = [("32x32/4 span 1", (5, 0, 3), 200), ("32x32/4 span 1 once", (20, 30, 1), 700), ("128x128/2 span 1", (700, 0, 800), 1500), ("tile", (2500, 60), 3300),
                    ("64x64/4 span 1 once", (1,) * 40, 1700)]
+
+# A block whose projection and experts' products all go in tiles of 256 x 256, more than the 256 compute units:
+# T tokens to K of E experts, H values, F inner ones, Q columns of the projection.
+TILED_BLOCK = dict(T=4096, K=2, E=4, H=2000, F=2304, Q=4400)

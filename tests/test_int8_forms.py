@@ -30,6 +30,14 @@ def test_longest_sums(rules):
         assert rules.experts(sum(counts), N, 131071, len(counts), sum(counts), 1, False) == form, (counts, N)
 
 
+def test_a_block_in_tiles(rules):
+    T, K, E, H, F, Q = (forms.TILED_BLOCK[k] for k in "TKEHFQ")
+    tiles = lambda m, n: -(-m // 256) * -(-n // 256)
+    assert rules.product(T, Q, H) == "tile" and tiles(T, Q) > 256
+    assert rules.experts(T * K, F, H, E, T, K, True) == "tile" and tiles(T * K, F) > 256
+    assert rules.experts(T * K, H, F, E, T * K, 1, False) == "tile" and tiles(T * K, H) >= 256
+
+
 def test_no_form_is_left_out(rules):
     """Every form of sizes spread over the whole range (over their logarithms)."""
     rng = random.Random(0)
