@@ -696,8 +696,9 @@ fo_status fo_quantize_rows(int32_t dtype, int64_t M, int64_t N, const void* x, i
  * way; rstd [M] fp32, for the backward pass. y, or codes and scales, is asked for (of N = 0
  * scales alone are written). h and y may each be x or residual (same ld); the outputs must
  * not overlap anything else.
- * Magnitudes of h up to 2^60 stay within fp32; products h * gamma are taken as fp32
- * holds them (exact from 2^-126 to 2^128).
+ * Magnitudes of h up to 2^60 stay within fp32, and rows whose largest is 2^-50 (below that
+ * an eps has to outweigh them); products h * gamma are taken as fp32 holds them (exact
+ * from 2^-126 to 2^128).
  * Errors: FO_ERR_ARG, FO_ERR_UNSUPPORTED, FO_ERR_SHAPE, FO_ERR_HIP.
  */
 fo_status fo_norm_add_forward(int32_t dtype, int64_t M, int64_t N, const void* x, int64_t ldx, const void* residual,
