@@ -666,9 +666,10 @@ fo_status fo_route_combine_backward(int32_t dtype, int64_t T, int32_t K, int64_t
  *
  * A matrix of N columns in 8 bits is int8 codes in rows `ld` bytes apart (a multiple
  * of 16, at least fo_int8_row_bytes(N), at most 2^22; 16-byte aligned), with an fp32
- * scale for each row: value = code * scale. Codes behind a row's end, up to
- * fo_int8_row_bytes(N) (N rounded up to a multiple of 16), are zeros. Products are fastest
- * where rows begin at multiples of 128 bytes (ld a multiple of 128, whatever N is).
+ * scale for each row: value = code * scale (signed codes, no zero point). Codes behind a
+ * row's end, up to fo_int8_row_bytes(N) (N rounded up to a multiple of 16), are zeros.
+ * Products are fastest where rows begin at multiples of 128 bytes (ld a multiple of 128,
+ * whatever N is).
  */
 
 int64_t fo_int8_row_bytes(int64_t N);

@@ -715,7 +715,9 @@ class _Args:
     def codes(self, x, M: int, N: int, ld, what: str):
         """(pointer, row distance) of a [M, N] matrix in 8 bits, each of its rows a whole number
         of 16 bytes: of shape [.., N] or, padded, [.., int8_row_bytes(N)] (dimensions ahead of
-        the last one together hold the rows), or one-dimensional storage."""
+        the last one together hold the rows), or one-dimensional storage. A uint8 tensor is a
+        container of the same bytes, as a 16-bit integer tensor is one of values: 255 is code -1,
+        and codes counted from a zero point are not taken for what they stand for."""
         width = -(-N // 16) * 16
         if x is None:
             return None, width

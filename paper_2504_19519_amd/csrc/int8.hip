@@ -31,7 +31,7 @@ namespace {
 // chunk c of row r at slot c ^ ((r / 2) % 8): 16 rows' chunks lie on different banks. ONCE:
 // the weights' loads are past the caches' keeping.
 // Bound by the weights' bytes where rows are few (16 tokens to 8 of 256 experts, 2048 x 7168:
-// 157 us, 6.3 TB/s), else by waits for LDS and by MFMAs (1024 x 4096 x 4096 21 us, 1.6 POPS).
+// 157 us, 6.3 TB/s), else by waits for LDS and by MFMAs (1024 x 4096 x 4096 22 us, 1.55 POPS).
 constexpr int kNontemporal = 2;         // cache policy of a buffer load
 template <int DT, int BM, int BN, int ST, bool EXPERTS, bool ONCE>
 __global__ __launch_bounds__(256, BM == 32 ? 4 : ST == 3 && BN == 128 ? 1 : 2) void int8_block_kernel(const Int8Args a) {

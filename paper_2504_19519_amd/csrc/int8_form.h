@@ -62,9 +62,9 @@ inline int64_t blocks_ns(int64_t blocks, int64_t steps) {
 // 4096 x 4096 of 64 15.8, of 128 25, of 128 x 64 13.8; 333 x 2881 x 1985 of 64 12.0, of 128 x 64
 // 10.3; 1024 x 2048 x 7168 26 and 21, but 256 x 4096 x 4096, where those of 64 are one to a compute
 // unit, 9.8 and 12.9; 128 x 4096 x 4096 of 32 9.4, of 64 9.5, of 64 x 32 8.7, 64 x 8192 x 1024 5.0,
-// 4.9 and 4.6, 256 x 4096 x 4096 15.5, 10.6 and 12.3; 16 x 14336 x 4096 of 32 11.3, of 64 12.0. In parts: 16 x 256 x 16384 8.7 for 16.0, 128 x 1024 x 16384
-// 13.1 for 18.5, but 16 x 256 x 4096 6.7 for 6.4, 1 x 4096 x 16384 15.8 for 12.0 in the kernel for
-// few blocks.
+// 4.9 and 4.6, 256 x 4096 x 4096 15.5, 10.6 and 12.3; 16 x 14336 x 4096 of 32 11.3, of 64 12.0. In
+// parts: 16 x 256 x 16384 8.7 for 16.0, 128 x 1024 x 16384 13.1 for 18.5, but 16 x 256 x 4096 6.7 for
+// 6.4, 1 x 4096 x 16384 15.8 for 12.0 in the kernel for few blocks.
 inline Int8Form product_form(int64_t M, int64_t N, int64_t K) {
     const int64_t steps = (int8_row_bytes(K) + 127) / 128;
     const auto blocks = [&](int64_t size) { return ((M + size - 1) / size) * ((N + size - 1) / size); };

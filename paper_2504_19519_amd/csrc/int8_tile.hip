@@ -13,10 +13,11 @@
 // tiles are a workgroup's is fixed by the counts: experts' tiles of unequal height leave some
 // workgroups more to do, but each finds its next tile and rows during the one before (8192
 // tokens to 8 of 128 experts, 2880x1440: 427 us; a workgroup per tile 476).
-// 8192x8192x8192 393 us, 2.8 POPS: the clock is power-limited (1.9 of 2.4 GHz), and the order
-// of reads and loads within a step makes no difference. Experts of 512 rows each, 2048x7168: 2.2
-// POPS, a tile's weights coming from memory, not from the caches; loads past the caches'
-// keeping help where one tile reads an expert's weights (256 rows each 512 -> 451 us), and cost as
+// 8192x8192x8192 403 us, 2.7 POPS. 8192x8192x3584: the matrix units are busy for 58 % of the cycles,
+// 8192x14336x4096 63 %; the power limit leaves 1.85 to 2.0 of 2.4 GHz. A step's 128 MFMAs a wave take
+// 2048 cycles of the about 2900 between its barriers, and the order of its reads and loads makes no
+// difference. Experts of 512 rows each, 2048x7168: 2.2 POPS, of as many on average 1.9 (48 % busy), a
+// tile's weights coming from memory, not from the caches; loads past the caches' keeping help where one tile reads an expert's weights (256 rows each 512 -> 451 us), and cost as
 // much where three do (528 rows each 539 -> 567): not taken.
 #include <hip/hip_runtime.h>
 

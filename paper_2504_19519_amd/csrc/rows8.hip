@@ -13,8 +13,8 @@
 // of exact arithmetic (codes_of).
 //
 // bf16: 8192x14336 to codes 62 us (5.7 TB/s); the norm of 16384x4096 to 16 bits 86 us and its
-// backward pass 87 (6.3 TB/s), the norm of 8192x4096 to h and codes 41 (6.3). A copy of 1 GiB
-// reaches 6.25 TB/s.
+// backward pass 86 (6.2 and 6.3 TB/s), the norm of 8192x4096 to h and codes 41 (5.7). A copy of
+// 1 GiB reaches 6.25 TB/s.
 //
 // Rows end anywhere: the thread with a row's last chunk of eight takes the row's last
 // eight values instead, some of them a second time. It writes what their own thread
